@@ -498,6 +498,103 @@ hch_status hch_pool_relu_bwd_pooled(const hch_levels *levels, int32_t level_in, 
 hch_status hch_relu_fwd(const float *x, float *y, int64_t n, void *stream);
 hch_status hch_relu_bwd(const float *y, const float *dy, float *dx, int64_t n, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * An attention block over the voxels of a level: layer norm, rotary positions, attention inside each
+ * shape.  Rows are voxels, voxel-major as everywhere; the linear layers between them are convolutions with
+ * F = 1 (hch_sconv_*).  16-bit tensors are bfloat16 bit patterns; sums, statistics and softmax are kept in fp32
+ * and rounded once, when an output is stored.  Every call is asynchronous on `stream`, allocates nothing and
+ * gives the same bits in every run.  Nothing is written on error.
+ * --------------------------------------------------------------------------------------------- */
+
+/*
+ * Layer norm over the c channels of a row, with a residual sum in front of it:
+ *   s = x + r;  y = (s - mean(s)) / sqrt(var(s) + eps) * gamma + beta     (var: biased)
+ *   X, R, S  DEVICE [n][c] of x_dtype.  R, S: both NULL (s = x), or R is read and S written; S may be X or R
+ *   gamma, beta  DEVICE [c] float, each may be NULL (1, 0)
+ *   Y        DEVICE [n][c] of y_dtype
+ *   stats    DEVICE [n][2] float: mean and 1 / sqrt(var + eps) of each row, for the backward pass; may be NULL
+ * y comes from the sum in fp32, before S is rounded to x_dtype.
+ * Backward, from the rows that were normalised (S, or X where there was no R) and their stats:
+ *   dX = gradient through the norm + dS       dS, dX  DEVICE [n][c] of x_dtype; dS (the gradient that
+ *                                             reaches s on the residual path) may be NULL; dX may be dS
+ *   dgamma, dbeta  DEVICE [c] float, overwritten; both NULL: not computed, and no workspace needed
+ *   workspace      DEVICE, 256-byte aligned, hch_layernorm_workspace_bytes(n, c) bytes (0 on bad arguments)
+ * n = 0 is allowed (dgamma = dbeta = 0).  Errors: HCH_EINVAL (null pointer, one of a pair alone, n < 0, c <= 0, eps
+ * negative or NaN, unknown dtype, workspace misaligned), HCH_EUNSUPPORTED (c > 8192), HCH_EWORKSPACE, HCH_EHIP.
+ */
+hch_status hch_layernorm_fwd(hch_dtype x_dtype, const void *X, const void *R, void *S, const float *gamma,
+                             const float *beta, hch_dtype y_dtype, void *Y, float *stats, int64_t n, int32_t c,
+                             float eps, void *stream);
+size_t hch_layernorm_workspace_bytes(int64_t n, int32_t c);
+hch_status hch_layernorm_bwd(hch_dtype x_dtype, const void *X, const float *stats, const float *gamma,
+                             hch_dtype dy_dtype, const void *dY, const void *dS, void *dX, float *dgamma,
+                             float *dbeta, int64_t n, int32_t c, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Rotary positions with three axes, from voxel coordinates.  A row holds `heads` heads of head_dim channels; in the
+ * first rot_heads of them channels (2p, 2p+1) = (a, b) become (a cos t - b sin t, a sin t + b cos t).  The pairs of a
+ * head are dealt to x, y, z in runs of sections[0], sections[1], sections[2]; pair j of an axis turns by
+ *   t = scale * coordinate * base^(-j / sections[axis]).
+ * The other heads, and pairs beyond the sections, are copied: so one call takes a packed row of queries, keys and
+ * values, and converts it where x_dtype and y_dtype differ.
+ *   X       DEVICE [n] rows of x_dtype, ld_x elements apart; Y the same of y_dtype, ld_y apart; X = Y is
+ *           allowed with one type and one stride
+ *   coords  DEVICE [n][3] int32 (hch_level_desc.coords is one); may be NULL if nothing turns
+ *   sections  HOST [3]
+ * hch_rope_bwd takes the gradient back through it (turns by -t).
+ * Errors: HCH_EINVAL (null pointer, head_dim odd, sizes negative, sections beyond head_dim / 2 pairs, strides
+ * below heads * head_dim, base <= 0, base or scale not finite, unknown dtype), HCH_EUNSUPPORTED (head_dim > 256,
+ * more than 2^31 workgroups), HCH_EHIP.
+ */
+hch_status hch_rope_fwd(hch_dtype x_dtype, const void *X, int64_t ld_x, hch_dtype y_dtype, void *Y, int64_t ld_y,
+                        const int32_t *coords, int64_t n, int32_t heads, int32_t rot_heads, int32_t head_dim,
+                        const int32_t *sections, float base, float scale, void *stream);
+hch_status hch_rope_bwd(hch_dtype dy_dtype, const void *dY, int64_t ld_dy, hch_dtype dx_dtype, void *dX,
+                        int64_t ld_dx, const int32_t *coords, int64_t n, int32_t heads, int32_t rot_heads,
+                        int32_t head_dim, const int32_t *sections, float base, float scale, void *stream);
+
+/*
+ * Attention inside each shape of a ragged batch.  Query row i of shape b and query head h sees the keys j of
+ * that shape whose mask is set, through key / value head h / (heads_q / heads_kv):
+ *   p_ij = softmax over j of (scale * q_i . k_j);   o_i = sum_j p_ij v_j;   lse_i = log sum_j exp(scale * q_i . k_j)
+ * A row that sees no key gets o = 0 and lse = -inf, and takes no part in any gradient.  What the mask leaves
+ * out, and rows of other shapes, are never part of a result, whatever they hold (NaN and infinity included).
+ *   q_offsets, k_offsets  DEVICE [batch + 1] int32, from 0 to n_q (n_k), not descending: shape b owns the rows
+ *             offsets[b] .. offsets[b+1]-1.  The same array for both is attention of a shape's voxels among
+ *             themselves; one query per shape pools it.  Empty shapes are allowed.  Values outside [0, n]
+ *             are taken as the nearer end; results for rows that no shape owns are undefined
+ *   key_mask  DEVICE [n_k] bytes, nonzero = seen; NULL: all
+ *   Q, O, dO, dQ  DEVICE [n_q] rows of heads_q * head_dim elements;  K, V, dK, dV  DEVICE [n_k] rows of
+ *             heads_kv * head_dim; each with a row stride of its own (ld_*, in elements), so they may be parts of
+ *             packed rows.  All of `dtype`
+ *   lse       DEVICE [n_q][heads_q] float; the forward call may leave it out (NULL), the backward call reads it
+ *   workspace DEVICE, 256-byte aligned, hch_attn_workspace_bytes(desc, kind) bytes: HCH_WS_FWD for hch_attn_fwd,
+ *             HCH_WS_BWD_DATA for hch_attn_bwd (0 on bad arguments, at least 256); only the sizes of the
+ *             description count
+ * hch_attn_bwd recomputes the probabilities from Q, K and lse and overwrites dQ, dK, dV; its O and lse are
+ * hch_attn_fwd's.  Any head_dim from 1 to 128; multiples of 16 bytes in head_dim, strides and addresses are faster.
+ * Errors: HCH_EINVAL (null pointer, negative size, heads_q not a multiple of heads_kv, scale not positive and
+ * finite, strides below a row's length, unknown dtype, workspace misaligned), HCH_EUNSUPPORTED (head_dim > 128,
+ * strides of 2^22 elements or more, n_q * heads_q or n_k beyond 2^31 - 1), HCH_EWORKSPACE, HCH_EHIP.
+ */
+typedef struct {
+    hch_dtype dtype;
+    int32_t batch, heads_q, heads_kv, head_dim;
+    float scale;
+    int64_t n_q, n_k;
+    const int32_t *q_offsets, *k_offsets;
+    const uint8_t *key_mask;
+    int64_t ld_q, ld_k, ld_v, ld_o;
+    int64_t ld_do, ld_dq, ld_dk, ld_dv;    /* hch_attn_bwd only */
+} hch_attn_desc;
+
+size_t hch_attn_workspace_bytes(const hch_attn_desc *desc, hch_ws_kind kind);
+hch_status hch_attn_fwd(const hch_attn_desc *desc, const void *Q, const void *K, const void *V, void *O, float *lse,
+                        void *workspace, size_t ws_bytes, void *stream);
+hch_status hch_attn_bwd(const hch_attn_desc *desc, const void *Q, const void *K, const void *V, const void *O,
+                        const float *lse, const void *dO, void *dQ, void *dK, void *dV, void *workspace,
+                        size_t ws_bytes, void *stream);
+
 /*
  * Measurement aid: a kernel that does nothing but matrix instructions, so that a benchmark can
  * state the rate the chip's matrix pipes actually reach next to the rates of the products above.

@@ -21,6 +21,8 @@ __all__ = [
     "hch_sconv_bwd_data", "hch_avgpool_fwd", "hch_avgpool_bwd", "hch_build_levels_ratios",
     "hch_spool_max_fwd", "hch_spool_max_bwd", "hch_spool_avg_fwd", "hch_spool_avg_bwd", "hch_build_tap_major",
     "hch_conv_bwd_weight_noalloc", "HCH_NOALLOC_SCRATCH_BYTES", "hch_probe_mfma", "hch_set_lean_loops",
+    "hch_layernorm_fwd", "hch_layernorm_workspace_bytes", "hch_layernorm_bwd", "hch_rope_fwd", "hch_rope_bwd",
+    "hch_attn_workspace_bytes", "hch_attn_fwd", "hch_attn_bwd",
 ]
 
 HCH_F32, HCH_BF16 = 0, 1
@@ -44,6 +46,8 @@ exported_symbols = [
     "hch_spool_max_fwd", "hch_spool_max_bwd", "hch_spool_avg_fwd", "hch_spool_avg_bwd", "hch_build_tap_major",
     "hch_conv_bwd_weight_noalloc",
     "hch_probe_mfma", "hch_set_lean_loops",
+    "hch_layernorm_fwd", "hch_layernorm_workspace_bytes", "hch_layernorm_bwd", "hch_rope_fwd", "hch_rope_bwd",
+    "hch_attn_workspace_bytes", "hch_attn_fwd", "hch_attn_bwd",
 ]
 
 
@@ -68,6 +72,14 @@ class _Desc(C.Structure):
 class _KernelStats(C.Structure):
     _fields_ = [("launches", C.c_int64), ("ms", C.c_double), ("bytes", C.c_double),
                 ("flops", C.c_double)]
+
+
+class _AttnDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("batch", C.c_int32), ("heads_q", C.c_int32), ("heads_kv", C.c_int32),
+                ("head_dim", C.c_int32), ("scale", C.c_float), ("n_q", C.c_int64), ("n_k", C.c_int64),
+                ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p), ("key_mask", C.c_void_p),
+                ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_v", C.c_int64), ("ld_o", C.c_int64),
+                ("ld_do", C.c_int64), ("ld_dq", C.c_int64), ("ld_dk", C.c_int64), ("ld_dv", C.c_int64)]
 
 
 _lib = None
@@ -129,6 +141,16 @@ def load_library():
     L.hch_pool_relu_bwd_pooled.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp]
     L.hch_relu_fwd.argtypes = [vp, vp, i64, vp]
     L.hch_relu_bwd.argtypes = [vp, vp, vp, i64, vp]
+    L.hch_layernorm_fwd.argtypes = [C.c_int, vp, vp, vp, vp, vp, C.c_int, vp, vp, i64, i32, C.c_float, vp]
+    L.hch_layernorm_workspace_bytes.argtypes = [i64, i32]
+    L.hch_layernorm_workspace_bytes.restype = sz
+    L.hch_layernorm_bwd.argtypes = [C.c_int, vp, vp, vp, C.c_int, vp, vp, vp, vp, vp, i64, i32, vp, sz, vp]
+    for name in ("hch_rope_fwd", "hch_rope_bwd"):
+        getattr(L, name).argtypes = [C.c_int, vp, i64, C.c_int, vp, i64, vp, i64, i32, i32, i32, vp, C.c_float, C.c_float, vp]
+    L.hch_attn_workspace_bytes.argtypes = [C.POINTER(_AttnDesc), C.c_int]
+    L.hch_attn_workspace_bytes.restype = sz
+    L.hch_attn_fwd.argtypes = [C.POINTER(_AttnDesc), vp, vp, vp, vp, vp, vp, sz, vp]
+    L.hch_attn_bwd.argtypes = [C.POINTER(_AttnDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.hch_probe_mfma.argtypes = [C.c_int, i32, i32, vp, vp]
     L.hch_set_lean_loops.argtypes = [i32]
     L.hch_set_lean_loops.restype = i32
@@ -279,6 +301,16 @@ class Levels:
         if level not in self._n:
             self._n[level] = int(self.info(level).n_total)
         return self._n[level]
+
+    def device_offsets(self, level):
+        """First row of each shape of `level`, and behind the last: [batch + 1] int32 on the GPU, as hch_attn_* take it."""
+        import torch
+        return torch.from_numpy(self.info(level).N.astype(np.int32)).cuda()
+
+    def device_positions(self, level):
+        """Voxel positions of `level` in data order, [n][3] int32 on the GPU, as hch_rope_* take them."""
+        import torch
+        return torch.from_numpy(self.info(level).coords_host()).cuda()
 
     def free(self):
         if self._h:
@@ -631,6 +663,120 @@ def hch_relu_fwd(x, y, n, stream=None):
 def hch_relu_bwd(y, dy, dx, n, stream=None):
     _check(load_library().hch_relu_bwd(_dp(y, "y", _F32, n), _dp(dy, "dy", _F32, n), _dp(dx, "dx", _F32, n), n,
                                        _stream(stream)))
+
+
+def hch_layernorm_fwd(x_dtype, X, R, S, gamma, beta, y_dtype, Y, stats, n, c, eps=1e-5, stream=None):
+    """s = X + R (kept in S; both None: s = X), Y = norm(s) * gamma + beta, stats = mean and 1 / deviation per row."""
+    tx, ty, e = _in_dtype(x_dtype), _in_dtype(y_dtype), n * c
+    _check(load_library().hch_layernorm_fwd(tx, _dp(X, "X", tx, e), _dp(R, "R", tx, e), _dp(S, "S", tx, e),
+                                            _dp(gamma, "gamma", _F32, c), _dp(beta, "beta", _F32, c), ty,
+                                            _dp(Y, "Y", ty, e), _dp(stats, "stats", _F32, 2 * n), n, c, eps,
+                                            _stream(stream)))
+
+
+def hch_layernorm_workspace_bytes(n, c):
+    return int(load_library().hch_layernorm_workspace_bytes(n, c))
+
+
+def hch_layernorm_bwd(x_dtype, X, stats, gamma, dy_dtype, dY, dS, dX, dgamma, dbeta, n, c, workspace, stream=None):
+    """Gradients of hch_layernorm_fwd from the rows it normalised and their stats; dX = that of the norm + dS."""
+    tx, ty, e = _in_dtype(x_dtype), _in_dtype(dy_dtype), n * c
+    _check(load_library().hch_layernorm_bwd(tx, _dp(X, "X", tx, e), _dp(stats, "stats", _F32, 2 * n),
+                                            _dp(gamma, "gamma", _F32, c), ty, _dp(dY, "dY", ty, e),
+                                            _dp(dS, "dS", tx, e), _dp(dX, "dX", tx, e),
+                                            _dp(dgamma, "dgamma", _F32, c), _dp(dbeta, "dbeta", _F32, c), n, c,
+                                            _dp(workspace, "workspace"), _nbytes(workspace), _stream(stream)))
+
+
+def _rows(t, what, dtype, n, width):
+    """Address and row stride of n rows of `width` elements: a 2-D tensor, or a part of the columns of one."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise HchError(1, f"{what}: must be a torch tensor in GPU memory")
+    if t.dtype != torch.float32 if dtype == HCH_F32 else t.element_size() != 2:
+        raise HchError(1, f"{what}: wrong element type {t.dtype}")
+    if t.dim() != 2 or t.shape[0] < n or t.shape[1] < width:
+        raise HchError(1, f"{what}: needs {n} rows of {width} elements, has {tuple(t.shape)}")
+    ld, step = t.stride()
+    if n == 0:
+        return t.data_ptr(), width
+    if (step != 1 and width > 1) or (n > 1 and ld < width):
+        raise HchError(1, f"{what}: the elements of a row must lie side by side and rows must not overlap")
+    return t.data_ptr(), ld if n > 1 else max(ld, width)
+
+
+def _rope(name, x_dtype, X, y_dtype, Y, coords, n, heads, rot_heads, head_dim, sections, base, scale, stream):
+    tx, ty, w = _in_dtype(x_dtype), _in_dtype(y_dtype), heads * head_dim
+    if len(sections) != 3:
+        raise HchError(1, "sections: the pairs of three axes")
+    x, ld_x = _rows(X, "first tensor", tx, n, w)
+    y, ld_y = _rows(Y, "second tensor", ty, n, w)
+    _check(getattr(load_library(), name)(tx, x, ld_x, ty, y, ld_y, _dp(coords, "coords", _I32, 3 * n), n, heads,
+                                         rot_heads, head_dim, (C.c_int32 * 3)(*sections), base, scale, _stream(stream)))
+
+
+def hch_rope_fwd(x_dtype, X, y_dtype, Y, coords, n, heads, rot_heads, head_dim, sections, base=10000.0, scale=1.0,
+                 stream=None):
+    """Rotary positions from coords [n][3]; X and Y are [n][heads * head_dim], or columns of wider rows."""
+    _rope("hch_rope_fwd", x_dtype, X, y_dtype, Y, coords, n, heads, rot_heads, head_dim, sections, base, scale, stream)
+
+
+def hch_rope_bwd(dy_dtype, dY, dx_dtype, dX, coords, n, heads, rot_heads, head_dim, sections, base=10000.0, scale=1.0,
+                 stream=None):
+    _rope("hch_rope_bwd", dy_dtype, dY, dx_dtype, dX, coords, n, heads, rot_heads, head_dim, sections, base, scale, stream)
+
+
+def hch_attn_workspace_bytes(kind, dtype, batch, n_q, n_k, heads_q, heads_kv, head_dim):
+    """kind: HCH_WS_FWD for hch_attn_fwd, HCH_WS_BWD_DATA for hch_attn_bwd."""
+    d = _AttnDesc(dtype=_in_dtype(dtype), batch=batch, heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim, n_q=n_q,
+                  n_k=n_k)
+    return int(load_library().hch_attn_workspace_bytes(C.byref(d), kind))
+
+
+def _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale, q_rows, k_rows):
+    """Description and addresses; q_rows / k_rows: names and tensors shaped like the queries / the keys, each of which
+    gives its stride to ld_<name>."""
+    import torch
+    dt = _in_dtype(dtype)
+    for t, what in ((Q, "Q"), (K, "K")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2:
+            raise HchError(1, f"{what}: must be a torch tensor of rows")
+    n_q, n_k = Q.shape[0], K.shape[0]
+    batch = q_offsets.numel() - 1
+    if batch < 0 or k_offsets.numel() != q_offsets.numel():
+        raise HchError(1, "q_offsets and k_offsets: batch + 1 entries each")
+    d = _AttnDesc(dtype=dt, batch=batch, heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim, scale=scale, n_q=n_q, n_k=n_k,
+                  q_offsets=_dp(q_offsets, "q_offsets", _I32).value, k_offsets=_dp(k_offsets, "k_offsets", _I32).value)
+    if key_mask is not None:
+        if key_mask.element_size() != 1:
+            raise HchError(1, "key_mask: must have elements of one byte")
+        d.key_mask = _dp(key_mask, "key_mask", None, n_k).value
+    ptr = {}
+    for rows, n, w in ((q_rows, n_q, heads_q * head_dim), (k_rows, n_k, heads_kv * head_dim)):
+        for name, t in rows:
+            ptr[name], ld = _rows(t, name, dt, n, w)
+            setattr(d, "ld_" + name, ld)
+    return d, ptr
+
+
+def hch_attn_fwd(dtype, Q, K, V, O, lse, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale, workspace,
+                 stream=None):
+    """Attention inside each shape: Q, O are [n_q][heads_q * head_dim], K, V [n_k][heads_kv * head_dim], or columns of
+    wider rows; offsets [batch + 1] int32 on the device; lse [n_q][heads_q] float or None; key_mask [n_k] bytes or None."""
+    d, p = _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale,
+                      (("q", Q), ("o", O)), (("k", K), ("v", V)))
+    _check(load_library().hch_attn_fwd(C.byref(d), p["q"], p["k"], p["v"], p["o"], _dp(lse, "lse", _F32, d.n_q * heads_q),
+                                       _dp(workspace, "workspace"), _nbytes(workspace), _stream(stream)))
+
+
+def hch_attn_bwd(dtype, Q, K, V, O, lse, dO, dQ, dK, dV, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale,
+                 workspace, stream=None):
+    """Gradients of hch_attn_fwd, from its inputs, its O and its lse."""
+    d, p = _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale,
+                      (("q", Q), ("o", O), ("do", dO), ("dq", dQ)), (("k", K), ("v", V), ("dk", dK), ("dv", dV)))
+    _check(load_library().hch_attn_bwd(C.byref(d), p["q"], p["k"], p["v"], p["o"], _dp(lse, "lse", _F32, d.n_q * heads_q),
+                                       p["do"], p["dq"], p["dk"], p["dv"], _dp(workspace, "workspace"),
+                                       _nbytes(workspace), _stream(stream)))
 
 
 def hch_probe_mfma(dtype, iters, workgroups, sink, stream=None):

@@ -4,12 +4,18 @@ from __future__ import annotations
 import hashlib
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhch.so")
-SOURCES = ["hch_api.hip", "psh_build.cpp"]
-HEADERS = ["kernels.hip.hpp", "direct.hip.hpp", "gemm_bf16.hip.hpp", "split_wgrad.hip.hpp", "split_conv.hip.hpp", "conv_small.hip.hpp", "split_columns.hip.hpp", "split_dcol.hip.hpp", "split_field.hip.hpp", "conv_bf16.hip.hpp", "psh_device.hip.hpp", "occupancy.hip.hpp", "psh_build.hpp", "profile.hpp", os.path.join("..", "..", "include", "hch.h")]
+SOURCES = ["hch_api.hip", "psh_build.cpp", "norm_rope.hip", "attn_bf16.hip", "attn_f32.hip", "attn_api.hip"]
+# hch_api.hip, attn_bf16.hip: accumulators of the matrix instructions in ordinary VGPRs, updated in place: with
+# the default (AGPR) form the compiler copies every accumulator through VGPRs once per loop
+# iteration, which costs the bf16 kernels more issue slots than their matrix instructions
+VGPR_FORM = ("hch_api.hip", "attn_bf16.hip")
+HEADERS = ["kernels.hip.hpp", "direct.hip.hpp", "gemm_bf16.hip.hpp", "split_wgrad.hip.hpp", "split_conv.hip.hpp", "conv_small.hip.hpp", "split_columns.hip.hpp", "split_dcol.hip.hpp", "split_field.hip.hpp", "conv_bf16.hip.hpp", "psh_device.hip.hpp", "occupancy.hip.hpp", "psh_build.hpp", "profile.hpp", "api_common.hpp", "norm.hip.hpp", "rope.hip.hpp", "attn.hip.hpp", "attn_launch.hpp", os.path.join("..", "..", "include", "hch.h")]
 
 
 def hipcc():
@@ -38,18 +44,22 @@ def build_library(force=True, verbose=False):
     deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS]
     if not force and os.path.exists(LIB) and all(os.path.getmtime(LIB) >= os.path.getmtime(d) for d in deps):
         return LIB
-    cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           # keep the compiler from forming packed-fp32 instructions
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           # accumulators of the matrix instructions in ordinary VGPRs, updated in place: with the
-           # default (AGPR) form the compiler copies every accumulator through VGPRs once per loop
-           # iteration, which costs the bf16 kernels more issue slots than their matrix instructions
-           "-mllvm", "-amdgpu-mfma-vgpr-form",
-           "-Wall", "-Wno-unused-function", "-pthread",
-           "-o", LIB] + os.environ.get("HCH_EXTRA_HIPCC_FLAGS", "").split() + [os.path.join(CSRC, f) for f in SOURCES]
-    if verbose:
-        print(" ".join(cmd))
-    subprocess.check_call(cmd)
+    base = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+            # keep the compiler from forming packed-fp32 instructions
+            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+            "-Wall", "-Wno-unused-function", "-pthread"] + os.environ.get("HCH_EXTRA_HIPCC_FLAGS", "").split()
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd))
+        subprocess.check_call(cmd)
+
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, f + ".o") for f in SOURCES]
+        with ThreadPoolExecutor(max_workers=len(SOURCES)) as pool:
+            list(pool.map(run, [base + (["-mllvm", "-amdgpu-mfma-vgpr-form"] if f in VGPR_FORM else [])
+                                + ["-c", os.path.join(CSRC, f), "-o", o] for f, o in zip(SOURCES, objects)]))
+        run(base + ["-shared", "-o", LIB] + objects)
     return LIB
 
 

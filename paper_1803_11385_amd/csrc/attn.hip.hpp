@@ -1,0 +1,723 @@
+// Attention inside the shapes of a ragged batch, forward and backward, on the matrix instructions.
+//
+//   forward   s_ij = scale q_i.k_j;  o_i = sum_j exp(s_ij - m_i) v_j / l_i with the running maximum m and sum l
+//             of the keys seen so far: one pass over the keys, no score goes to memory
+//   backward  p_ij = exp(s_ij - lse_i);  D_i = dO_i . o_i;  dS_ij = p_ij (dO_i . v_j - D_i)
+//             dV_j = sum_i p_ij dO_i;  dK_j = scale sum_i dS_ij q_i;  dQ_i = scale sum_j dS_ij k_j
+//
+// All kernels multiply 32 x 32 tiles with the 32x32 instructions (bf16: 16 terms, fp32: 2 terms at a time).  The
+// scores are always formed so that what stays fixed for a wavefront (its queries, or in the pass over keys its keys)
+// is the column, i.e. the lane, and what streams past is the row, i.e. the register.  Then
+//   * a row's maximum and sum are sums over a lane's own registers and one exchange between the two
+//     half-wavefronts, and what scales a query is one number per lane;
+//   * the probabilities are already laid out as the right operand of the second product, whose reduction runs
+//     over the streamed rows: register r of half h is row 8 (r / 4) + 4 h + r % 4, and the left operand is read
+//     in the same order, so nothing is exchanged between the products.
+// The streamed tile lies row by row in LDS, 16 bytes between rows: ds_read_b128 for products over the channels
+// (rows of 16 consecutive bytes), for products over the rows with bf16 the transposing ds_read_b64_tr_b16 (16
+// lanes give the addresses of 4 rows x 16 channels and get 4 rows of one channel each), with fp32 plain
+// reads across the lanes.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace hch {
+namespace attn {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr int SRD3 = 0x00020000, OUT = 0x7fffffff;      // raw buffer descriptor; an offset past every buffer
+
+struct Args {
+    const void *Q, *K, *V, *O, *dO;
+    void *Ow, *dQ, *dK, *dV;               // outputs
+    float *lse;                            // [n_q][hq]
+    const int32_t *qo, *ko;                // [batch + 1]
+    const uint8_t *mask;                   // [n_k] or null
+    float *part;                           // [splits][n_q * hq][d] sums of a split over the keys
+    float2 *ml;                            // [splits][n_q * hq]    their maximum and sum
+    float *delta;                          // [n_q * hq] D
+    int64_t nq, nk, ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
+    int batch, hq, hkv, group, d;
+    int slots, splits, total;              // tiles per head at most, splits over the streamed rows, slots * heads * splits
+    int vec;                               // everything in 16-byte pieces
+    float scale, c;                        // c = scale log2(e)
+};
+
+// ---------------------------------------------------------------------------------------------
+// types
+// ---------------------------------------------------------------------------------------------
+template <typename T> struct Mma;
+template <> struct Mma<__bf16> {
+    static constexpr int E = 8;            // elements of 16 bytes
+    // acc += A B over the channels of one 16-byte piece of both halves
+    static __device__ __forceinline__ f32x16 rows(u32x4 a, u32x4 b, f32x16 acc)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+    }
+    struct Col { bf16x8 v; };              // 16 streamed rows of the right operand
+    static __device__ __forceinline__ Col col(const f32x16 &p, int s)
+    {
+        Col c;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c.v[j] = (__bf16)p[8 * s + j];
+        return c;
+    }
+    // byte offset of this lane's piece of the left operand in a tile with rows of `stride` bytes
+    static __device__ __forceinline__ int left_offset(int lane, int stride)
+    {
+        return (4 * (lane >> 5) + ((lane & 15) >> 2)) * stride + (16 * ((lane >> 4) & 1) + (lane & 3) * 4) * 2;
+    }
+    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int s, int dt, Col b, f32x16 acc)
+    {
+        const char *p = tile + 16 * s * stride + 64 * dt;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)p);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)(p + 8 * stride));
+        const auto a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b.v, acc, 0, 0, 0);
+    }
+};
+template <> struct Mma<float> {
+    static constexpr int E = 4;
+    static __device__ __forceinline__ f32x16 rows(u32x4 a, u32x4 b, f32x16 acc)
+    {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], y[j], acc, 0, 0, 0);
+        return acc;
+    }
+    struct Col { float v[8]; };
+    static __device__ __forceinline__ Col col(const f32x16 &p, int s)
+    {
+        Col c;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c.v[j] = p[8 * s + j];
+        return c;
+    }
+    static __device__ __forceinline__ int left_offset(int lane, int stride) { return 4 * (lane >> 5) * stride + 4 * (lane & 31); }
+    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int s, int dt, Col b, f32x16 acc)
+    {
+        const char *p = tile + 16 * s * stride + 128 * dt;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float *)(p + (8 * (j / 4) + j % 4) * stride), b.v[j], acc, 0, 0, 0);
+        return acc;
+    }
+};
+
+// the other half-wavefront's value
+__device__ __forceinline__ float other_half(float v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float((threadIdx.x & 32) ? s[0] : s[1]);
+}
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// row of register r of a tile, less the 4 h of the half
+__device__ __forceinline__ constexpr int reg_row(int r) { return 8 * (r >> 2) + (r & 3); }
+
+// ---------------------------------------------------------------------------------------------
+// work distribution
+// ---------------------------------------------------------------------------------------------
+// Workgroups go to the 8 XCDs in turn; runs of RUN neighbours in the work list are kept on one, so that the tiles that
+// read the same keys share its L2, while shapes of different lengths still spread over all of them.
+constexpr int RUN = 16;
+__device__ __forceinline__ int work_item(int id) { return ((id >> 3) / RUN * 8 + (id & 7)) * RUN + (id >> 3) % RUN; }
+inline unsigned work_grid(int total) { return (unsigned)((total + 8 * RUN - 1) / (8 * RUN) * (8 * RUN)); }
+
+// A shape's rows [begin, end) of n, safe whatever the offsets hold.
+struct Span { int begin, end; };
+__device__ __forceinline__ int clamped(int32_t v, int64_t n) { return (int)max((int64_t)0, min((int64_t)v, n)); }
+__device__ __forceinline__ Span span_of(const int32_t *off, int b, int64_t n)
+{
+    Span s;
+    s.begin = __builtin_amdgcn_readfirstlane(clamped(off[b], n));
+    s.end = __builtin_amdgcn_readfirstlane(clamped(off[b + 1], n));
+    s.end = max(s.end, s.begin);
+    return s;
+}
+// Tiles of `size` rows are dealt to shapes without a sum over them: shape b's tiles have the slots from
+// floor(offset_b / size) + b on, which is room enough, as ceil(len / size) <= floor(end / size) - floor(begin / size) + 1.
+// Returns the shape of a slot (the last whose first slot is not beyond it), by 64-fold search.
+__device__ __forceinline__ int shape_of_slot(const int32_t *off, int batch, int64_t n, int rows_each, int size, int slot, int lane)
+{
+    int lo = 0, cnt = batch;
+    while (cnt > 1) {
+        const int step = (cnt + 63) >> 6, i = lane * step;
+        const bool in = i < cnt && (int64_t)clamped(off[lo + (i < cnt ? i : 0)], n) * rows_each / size + lo + i <= slot;
+        const int k = max(0, (int)__popcll(__ballot(in)) - 1);
+        lo += k * step;
+        cnt = min(step, cnt - k * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+__device__ __forceinline__ int first_slot(int begin, int rows_each, int size, int b) { return (int)((int64_t)begin * rows_each / size) + b; }
+inline int64_t slots_of(int64_t n, int rows_each, int size, int batch) { return n * rows_each / size + batch; }
+
+// ---------------------------------------------------------------------------------------------
+// tiles
+// ---------------------------------------------------------------------------------------------
+template <typename T, int D> struct Tile {
+    static constexpr int STRIDE = D * (int)sizeof(T) + 16, CHUNKS = D * (int)sizeof(T) / 32, DT = D / 32;
+};
+
+// 16 bytes from element 0 .. of a row, `have` of them there; zeros behind
+template <typename T> __device__ __forceinline__ u32x4 load_elements(__amdgpu_buffer_rsrc_t rs, int offset, int have)
+{
+    u32x4 v;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_raw_buffer_load_b32(rs, j < have ? offset + 4 * j : OUT, 0, 0);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, 2 * j < have ? offset + 4 * j : OUT, 0, 0);
+            const uint32_t hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, 2 * j + 1 < have ? offset + 4 * j + 2 : OUT, 0, 0);
+            v[j] = lo | hi << 16;
+        }
+    }
+    return v;
+}
+
+// The part of a tile of ROWS rows that a thread moves from memory to LDS: fixed pieces of 16 bytes.
+template <typename T, int D, int ROWS, int THREADS> struct Stage {
+    static constexpr int PER_ROW = D * (int)sizeof(T) / 16, PIECES = ROWS * PER_ROW, N = (PIECES + THREADS - 1) / THREADS;
+    u32x4 r[N];
+    // rows [row0, row0 + ROWS) of a matrix that ends before row `end`; `base`: channel 0 of row 0.  Rows and channels that
+    // do not exist come back as zeros, from the bounds of the descriptor.
+    __device__ __forceinline__ void load(const T *base, int64_t ld, int row0, int end, int d, bool vec, int tid)
+    {
+        const int rows = max(0, min(ROWS, end - row0));
+        const int bytes = rows ? (int)(((rows - 1) * ld + d) * (int)sizeof(T)) : 0;
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(base + row0 * ld), 0, bytes, SRD3);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = tid + i * THREADS, row = p / PER_ROW, e = (p - row * PER_ROW) * Mma<T>::E;
+            const int have = PIECES % THREADS && p >= PIECES ? 0 : d - e;
+            const int offset = (int)(row * ld + e) * (int)sizeof(T);
+            if (vec) r[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, have > 0 ? offset : OUT, 0, 0));
+            else r[i] = load_elements<T>(rs, offset, row < rows ? have : 0);
+        }
+    }
+    // bit `row` of keep[row / 64] clear: the row is written as zeros
+    __device__ __forceinline__ void store(char *tile, int tid, const uint64_t *keep)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = tid + i * THREADS, row = p / PER_ROW, col = p - row * PER_ROW;
+            if (PIECES % THREADS && p >= PIECES) continue;
+            u32x4 v = r[i];
+            if (keep && !(keep[row >> 6] >> (row & 63) & 1)) v = u32x4{0, 0, 0, 0};
+            *(u32x4 *)(tile + row * Tile<T, D>::STRIDE + col * 16) = v;
+        }
+    }
+};
+
+// A wavefront's own 32 rows as an operand of products over the channels: the pieces at bytes 32 s + 16 h of a row.
+template <typename T, int D> struct Own {
+    u32x4 v[Tile<T, D>::CHUNKS];
+    __device__ __forceinline__ void load(const T *row, bool valid, int d, bool vec, int h)
+    {
+#pragma unroll
+        for (int s = 0; s < Tile<T, D>::CHUNKS; ++s) {
+            const int e = (32 * s + 16 * h) / (int)sizeof(T);
+            u32x4 x = {0, 0, 0, 0};
+            if (valid && e < d) {
+                if (vec) x = *(const u32x4 *)(row + e);
+                else {
+                    T t[Mma<T>::E];
+#pragma unroll
+                    for (int j = 0; j < Mma<T>::E; ++j) t[j] = e + j < d ? row[e + j] : (T)0.f;
+                    __builtin_memcpy(&x, t, 16);
+                }
+            }
+            v[s] = x;
+        }
+    }
+};
+
+// scores of 32 streamed rows against the own rows
+template <typename T, int D> __device__ __forceinline__ f32x16 product(const char *tile, const Own<T, D> &own, int lane, f32x16 acc)
+{
+    const char *p = tile + (lane & 31) * Tile<T, D>::STRIDE + 16 * (lane >> 5);
+#pragma unroll
+    for (int s = 0; s < Tile<T, D>::CHUNKS; ++s) acc = Mma<T>::rows(*(const u32x4 *)(p + 32 * s), own.v[s], acc);
+    return acc;
+}
+// acc[dt] += (32 streamed rows, transposed) p
+template <typename T, int D>
+__device__ __forceinline__ void fold(const char *tile, const f32x16 &p, int left, f32x16 (&acc)[Tile<T, D>::DT])
+{
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const typename Mma<T>::Col b = Mma<T>::col(p, s);
+#pragma unroll
+        for (int dt = 0; dt < Tile<T, D>::DT; ++dt) acc[dt] = Mma<T>::cols(tile + left, Tile<T, D>::STRIDE, s, dt, b, acc[dt]);
+    }
+}
+// this lane's row of a result: channel 32 dt + 8 (r / 4) + 4 h + r % 4
+template <typename U, int DT>
+__device__ __forceinline__ void store_row(U *row, const f32x16 (&acc)[DT], float f, int d, bool vec, int h)
+{
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int e = 32 * dt + reg_row(r) + 4 * h;
+            if (e >= d) continue;
+            typedef U U4 __attribute__((ext_vector_type(4)));
+            U4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = (U)(acc[dt][r + j] * f);
+            if (vec) *(U4 *)(row + e) = v;
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (e + j < d) row[e + j] = v[j];
+        }
+}
+
+// Which of 64 keys from `key` on are there and seen.
+__device__ __forceinline__ int key_byte(const uint8_t *mask, int key, int end) { return key < end ? (mask ? (int)mask[key] : 1) : 0; }
+
+// Sizes of the passes over the keys.  QW wavefronts have rows of their own and KW = WAVES / QW share a row tile's keys:
+// 4 x 1 for long queries, 1 x 4 where a shape has few query rows and the keys are what there is to read.
+template <typename T, int D, int QW> struct Keys {
+    static constexpr int WAVES = QW == 1 && D * sizeof(T) > 256 ? 2 : 4, THREADS = 64 * WAVES, KW = WAVES / QW, BQ = 32 * QW;
+    static constexpr int BK = QW == 1 ? 32 * KW : sizeof(T) == 2 ? 64 : 32, NT = BK / 32 / KW;
+    static constexpr int BUFFERS = QW == 1 ? 1 : 2, TILE = BK * Tile<T, D>::STRIDE;
+    static constexpr int WORDS = (BK + 63) / 64;
+    static constexpr int LDS = 2 * BUFFERS * TILE;
+};
+
+// ---------------------------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------------------------
+// Query rows of the heads that share a key head are one list, row = token * group + (head within the group), so that
+// a tile of keys serves the whole group.
+template <typename T, int D, int QW>
+__global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_fwd_kernel(Args a)
+{
+    typedef Keys<T, D, QW> S;
+    typedef Tile<T, D> L;
+    __shared__ __align__(16) char lds[S::LDS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave : 0;
+    const int w = work_item(blockIdx.x);
+    if (w >= a.total) return;
+    const int split = w % a.splits, slot = w / a.splits % a.slots, kvh = w / a.splits / a.slots;
+    const int b = shape_of_slot(a.qo, a.batch, a.nq, a.group, S::BQ, slot, lane);
+    const Span q = span_of(a.qo, b, a.nq), k = span_of(a.ko, b, a.nk);
+    const int tile = slot - first_slot(q.begin, a.group, S::BQ, b);
+    const int64_t rows = (int64_t)(q.end - q.begin) * a.group, row0 = (int64_t)tile * S::BQ;
+    if (tile < 0 || row0 >= rows) return;
+
+    const int64_t row = row0 + 32 * qw + (lane & 31);
+    const bool valid = row < rows;
+    const int64_t token = valid ? q.begin + row / a.group : q.begin;
+    const int head = kvh * a.group + (valid ? (int)(row % a.group) : 0);
+    Own<T, D> own;
+    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, valid, a.d, a.vec, h);
+
+    const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
+    const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+    const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
+    const uint8_t *mask = a.mask ? a.mask + k.begin : nullptr;
+    const int len = k.end - k.begin;
+    const int left = Mma<T>::left_offset(lane, L::STRIDE);
+
+    f32x16 acc[L::DT];
+#pragma unroll
+    for (int dt = 0; dt < L::DT; ++dt) acc[dt] = f32x16{};
+    float m = -INFINITY, l = 0.f;
+
+    Stage<T, D, S::BK, S::THREADS> ks, vs;
+    int seen[S::WORDS];
+    auto load = [&](int t) {
+        ks.load(kp, a.ld_k, t * S::BK, len, a.d, a.vec, tid);
+        vs.load(vp, a.ld_v, t * S::BK, len, a.d, a.vec, tid);
+#pragma unroll
+        for (int i = 0; i < S::WORDS; ++i) seen[i] = key_byte(mask, t * S::BK + 64 * i + lane, len);
+    };
+    if (t0 < t1) load(t0);
+    for (int t = t0; t < t1; ++t) {
+        char *kt = lds + (S::BUFFERS == 2 ? (t & 1) * 2 * S::TILE : 0), *vt = kt + S::TILE;
+        uint64_t keep[S::WORDS];
+        bool all = true;
+#pragma unroll
+        for (int i = 0; i < S::WORDS; ++i) {
+            keep[i] = __ballot(seen[i] != 0);
+            all &= S::BK - 64 * i >= 64 ? keep[i] == ~0ull : (uint32_t)keep[i] == ~0u;
+        }
+        if (S::BUFFERS == 1) __syncthreads();
+        ks.store(kt, tid, nullptr);
+        if (all) vs.store(vt, tid, nullptr);
+        else vs.store(vt, tid, keep);                   // a value that is not seen may be anything: 0 * NaN
+        __syncthreads();
+        if (t + 1 < t1) load(t + 1);
+
+        f32x16 s[S::NT];
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < S::NT; ++i) {
+            const int sub = QW == 1 ? kw : i;
+            s[i] = product<T, D>(kt + 32 * sub * L::STRIDE, own, lane, f32x16{});
+            if (!all) {
+                const uint32_t bits = (uint32_t)(keep[sub >> 1] >> (32 * (sub & 1))) >> (4 * h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) if (!(bits >> reg_row(r) & 1)) s[i][r] = -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[i][r]);
+        }
+        top = fmaxf(top, other_half(top)) * a.c;
+        // The sums are kept relative to a maximum that is brought up only when a score exceeds it by 2^8: exact in
+        // fp32 either way (exponents have room), and nearly every tile is spared the scaling of the sums.
+        if (__any(top > m + 8.f)) {
+            const bool up = top > m + 8.f;
+            const float f = up ? exp2_fast(m - top) : 1.f;
+            if (up) m = top;
+            l *= f;
+#pragma unroll
+            for (int dt = 0; dt < L::DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[dt][r] *= f;
+        }
+        const float base = m == -INFINITY ? 0.f : m;    // no key yet: exp2(-inf) = 0, not -inf + inf
+#pragma unroll
+        for (int i = 0; i < S::NT; ++i) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[i][r] = exp2_fast(__builtin_fmaf(s[i][r], a.c, -base));
+                l += s[i][r];
+            }
+            fold<T, D>(vt + 32 * (QW == 1 ? kw : i) * L::STRIDE, s[i], left, acc);
+        }
+    }
+    l += other_half(l);
+
+    if constexpr (QW == 1) {                            // the wavefronts' shares of the keys, joined in LDS
+        __syncthreads();
+        constexpr int W = D + 4;                        // floats of a row: its sums, then maximum and sum of weights
+        float *mine = (float *)lds + (wave * 32 + (lane & 31)) * W;
+#pragma unroll
+        for (int dt = 0; dt < L::DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *(f32x4 *)(mine + 32 * dt + reg_row(r) + 4 * h) = f32x4{acc[dt][r], acc[dt][r + 1], acc[dt][r + 2], acc[dt][r + 3]};
+        if (h == 0) { mine[D] = m; mine[D + 1] = l; }
+        __syncthreads();
+        if (wave) return;
+        float f[S::KW];
+        const float *all = (const float *)lds + (lane & 31) * W;
+        m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < S::KW; ++i) m = fmaxf(m, all[i * 32 * W + D]);
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < S::KW; ++i) {
+            f[i] = m == -INFINITY ? 0.f : exp2_fast(all[i * 32 * W + D] - m);
+            l += f[i] * all[i * 32 * W + D + 1];
+        }
+#pragma unroll
+        for (int dt = 0; dt < L::DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < S::KW; ++i) t += f[i] * *(const f32x4 *)(all + i * 32 * W + 32 * dt + reg_row(r) + 4 * h);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[dt][r + j] = t[j];
+            }
+    }
+    if (!valid) return;
+    const int64_t at = token * a.hq + head;
+    if (a.splits == 1) {
+        store_row<T>((T *)a.Ow + token * a.ld_o + (int64_t)head * a.d, acc, l > 0.f || l != l ? 1.f / l : 0.f, a.d, a.vec, h);
+        if (a.lse && h == 0) a.lse[at] = l > 0.f || l != l ? m * LN2 + logf(l) : -INFINITY;
+    } else {
+        const int64_t p = (int64_t)split * a.nq * a.hq + at;
+        if (l > 0.f || l != l) store_row<float>(a.part + p * a.d, acc, 1.f, a.d, a.d % 4 == 0, h);
+        if (h == 0) a.ml[p] = make_float2(m, l);
+    }
+}
+
+// Joins the splits of a row: thread groups of 16 lanes over the channels, the splits dealt to the 16 groups of a workgroup.
+template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(Args a)
+{
+    __shared__ float sums[16][128];
+    __shared__ float2 ml[16];
+    const int64_t at = blockIdx.x, rows = a.nq * a.hq;
+    const int x = threadIdx.x & 15, g = threadIdx.x >> 4;
+    float m = -INFINITY;
+    for (int s = g; s < a.splits; s += 16) m = fmaxf(m, a.ml[s * rows + at].x);
+    float l = 0.f, acc[8] = {};
+    for (int s = g; s < a.splits; s += 16) {
+        const float2 v = a.ml[s * rows + at];
+        if (!(v.y > 0.f || v.y != v.y)) continue;       // a split without a key has written no sums
+        const float f = exp2_fast(v.x - m);
+        l += f * v.y;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (x + 16 * j < a.d) acc[j] += f * a.part[(s * rows + at) * a.d + x + 16 * j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[g][x + 16 * j] = acc[j];
+    if (x == 0) ml[g] = make_float2(m, l);
+    __syncthreads();
+    m = -INFINITY;
+    for (int i = 0; i < 16; ++i) m = fmaxf(m, ml[i].x);
+    l = 0.f;
+    for (int i = 0; i < 16; ++i) l += ml[i].y != 0.f ? ml[i].y * exp2_fast(ml[i].x - m) : 0.f;
+    const int64_t token = at / a.hq;
+    const int head = (int)(at - token * a.hq);
+    const bool some = l > 0.f || l != l;
+    if (threadIdx.x < a.d) {
+        float t = 0.f;
+        for (int i = 0; i < 16; ++i) if (ml[i].y != 0.f) t += sums[i][threadIdx.x] * exp2_fast(ml[i].x - m);
+        ((T *)a.Ow)[token * a.ld_o + (int64_t)head * a.d + threadIdx.x] = (T)(some ? t / l : 0.f);
+    }
+    if (a.lse && threadIdx.x == 0) a.lse[at] = some ? m * LN2 + logf(l) : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------------------------
+// backward
+// ---------------------------------------------------------------------------------------------
+// a . b of this lane's row: 16-byte pieces held by the two halves
+template <typename T, int D> __device__ __forceinline__ float row_dot(const Own<T, D> &a, const Own<T, D> &b)
+{
+    float t = 0.f;
+#pragma unroll
+    for (int s = 0; s < Tile<T, D>::CHUNKS; ++s) {
+        T x[Mma<T>::E], y[Mma<T>::E];
+        __builtin_memcpy(x, &a.v[s], 16);
+        __builtin_memcpy(y, &b.v[s], 16);
+#pragma unroll
+        for (int j = 0; j < Mma<T>::E; ++j) t += (float)x[j] * (float)y[j];
+    }
+    return t + other_half(t);
+}
+
+// dQ, and D for the pass over the keys: the walk of the forward kernel.
+template <typename T, int D, int QW>
+__global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_bwd_dq_kernel(Args a)
+{
+    typedef Keys<T, D, QW> S;
+    typedef Tile<T, D> L;
+    __shared__ __align__(16) char lds[S::LDS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave : 0;
+    const int w = work_item(blockIdx.x);
+    if (w >= a.total) return;
+    const int split = w % a.splits, slot = w / a.splits % a.slots, kvh = w / a.splits / a.slots;
+    const int b = shape_of_slot(a.qo, a.batch, a.nq, a.group, S::BQ, slot, lane);
+    const Span q = span_of(a.qo, b, a.nq), k = span_of(a.ko, b, a.nk);
+    const int tile = slot - first_slot(q.begin, a.group, S::BQ, b);
+    const int64_t rows = (int64_t)(q.end - q.begin) * a.group, row0 = (int64_t)tile * S::BQ;
+    if (tile < 0 || row0 >= rows) return;
+
+    const int64_t row = row0 + 32 * qw + (lane & 31);
+    const bool valid = row < rows;
+    const int64_t token = valid ? q.begin + row / a.group : q.begin;
+    const int head = kvh * a.group + (valid ? (int)(row % a.group) : 0);
+    const int64_t at = token * a.hq + head;
+    const float lse = a.lse[at];
+    const bool part = valid && lse != -INFINITY;        // a row that saw no key: its gradient is zero, whatever dO holds
+    const float lse2 = part ? lse * LOG2E : INFINITY;
+    Own<T, D> own, grad;
+    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, part, a.d, a.vec, h);
+    grad.load((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d, part, a.d, a.vec, h);
+    float delta;
+    {
+        Own<T, D> out;
+        out.load((const T *)a.O + token * a.ld_o + (int64_t)head * a.d, part, a.d, a.vec, h);
+        delta = row_dot<T, D>(grad, out);
+    }
+    if (valid && split == 0 && kw == 0 && h == 0) a.delta[at] = delta;
+
+    const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
+    const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
+    const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
+    const uint8_t *mask = a.mask ? a.mask + k.begin : nullptr;
+    const int len = k.end - k.begin;
+    const int left = Mma<T>::left_offset(lane, L::STRIDE);
+
+    f32x16 acc[L::DT];
+#pragma unroll
+    for (int dt = 0; dt < L::DT; ++dt) acc[dt] = f32x16{};
+    Stage<T, D, S::BK, S::THREADS> ks, vs;
+    int seen[S::WORDS];
+    auto load = [&](int t) {
+        ks.load(kp, a.ld_k, t * S::BK, len, a.d, a.vec, tid);
+        vs.load(vp, a.ld_v, t * S::BK, len, a.d, a.vec, tid);
+#pragma unroll
+        for (int i = 0; i < S::WORDS; ++i) seen[i] = key_byte(mask, t * S::BK + 64 * i + lane, len);
+    };
+    if (t0 < t1) load(t0);
+    for (int t = t0; t < t1; ++t) {
+        char *kt = lds + (S::BUFFERS == 2 ? (t & 1) * 2 * S::TILE : 0), *vt = kt + S::TILE;
+        uint64_t keep[S::WORDS];
+        bool all = true;
+#pragma unroll
+        for (int i = 0; i < S::WORDS; ++i) {
+            keep[i] = __ballot(seen[i] != 0);
+            all &= S::BK - 64 * i >= 64 ? keep[i] == ~0ull : (uint32_t)keep[i] == ~0u;
+        }
+        if (S::BUFFERS == 1) __syncthreads();
+        if (all) { ks.store(kt, tid, nullptr); vs.store(vt, tid, nullptr); }
+        else { ks.store(kt, tid, keep); vs.store(vt, tid, keep); }
+        __syncthreads();
+        if (t + 1 < t1) load(t + 1);
+#pragma unroll
+        for (int i = 0; i < S::NT; ++i) {
+            const int sub = QW == 1 ? kw : i;
+            f32x16 s = product<T, D>(kt + 32 * sub * L::STRIDE, own, lane, f32x16{});
+            f32x16 g;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] = -delta;
+            g = product<T, D>(vt + 32 * sub * L::STRIDE, grad, lane, g);
+            if (!all) {
+                const uint32_t bits = (uint32_t)(keep[sub >> 1] >> (32 * (sub & 1))) >> (4 * h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) if (!(bits >> reg_row(r) & 1)) s[r] = -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] *= exp2_fast(__builtin_fmaf(s[r], a.c, -lse2));
+            fold<T, D>(kt + 32 * sub * L::STRIDE, g, left, acc);
+        }
+    }
+    if constexpr (QW == 1) {
+        __syncthreads();
+        constexpr int W = D + 4;
+        float *mine = (float *)lds + (wave * 32 + (lane & 31)) * W;
+#pragma unroll
+        for (int dt = 0; dt < L::DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *(f32x4 *)(mine + 32 * dt + reg_row(r) + 4 * h) = f32x4{acc[dt][r], acc[dt][r + 1], acc[dt][r + 2], acc[dt][r + 3]};
+        __syncthreads();
+        if (wave) return;
+        const float *all = (const float *)lds + (lane & 31) * W;
+#pragma unroll
+        for (int dt = 0; dt < L::DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < S::KW; ++i) t += *(const f32x4 *)(all + i * 32 * W + 32 * dt + reg_row(r) + 4 * h);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[dt][r + j] = t[j];
+            }
+    }
+    if (!valid) return;
+    if (a.splits == 1) store_row<T>((T *)a.dQ + token * a.ld_dq + (int64_t)head * a.d, acc, a.scale, a.d, a.vec, h);
+    else store_row<float>(a.part + ((int64_t)split * a.nq * a.hq + at) * a.d, acc, a.scale, a.d, a.d % 4 == 0, h);
+}
+
+// dQ = the sum of its splits, in their order; a thread per element
+template <typename T> __global__ __launch_bounds__(256) void attn_bwd_join_kernel(Args a)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = a.nq * a.hq;
+    if (i >= rows * a.d) return;
+    float t = 0.f;
+    for (int s = 0; s < a.splits; ++s) t += a.part[s * rows * a.d + i];
+    const int64_t at = i / a.d, token = at / a.hq;
+    ((T *)a.dQ)[token * a.ld_dq + (at - token * a.hq) * a.d + (i - at * a.d)] = (T)t;
+}
+
+// dK and dV: a wavefront has 32 keys, the queries of all heads that share their head stream past, one head after
+// the other, so the sum over them is taken in registers in a fixed order.
+template <typename T, int D> struct Queries {
+    static constexpr int THREADS = 256, BK = 128, BR = sizeof(T) == 2 ? 64 : 32, NT = BR / 32, TILE = BR * Tile<T, D>::STRIDE;
+    static constexpr int BUFFER = 2 * TILE + 2 * BR * 4, LDS = 2 * BUFFER;
+};
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(Args a)
+{
+    typedef Queries<T, D> S;
+    typedef Tile<T, D> L;
+    __shared__ __align__(16) char lds[S::LDS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int w = work_item(blockIdx.x);
+    if (w >= a.total) return;
+    const int slot = w % a.slots, kvh = w / a.slots;
+    const int b = shape_of_slot(a.ko, a.batch, a.nk, 1, S::BK, slot, lane);
+    const Span q = span_of(a.qo, b, a.nq), k = span_of(a.ko, b, a.nk);
+    const int tile = slot - first_slot(k.begin, 1, S::BK, b);
+    if (tile < 0 || tile >= (k.end - k.begin + S::BK - 1) / S::BK) return;
+
+    const int64_t key = k.begin + (int64_t)tile * S::BK + 32 * wave + (lane & 31);
+    const bool valid = key < k.end, seen = valid && (!a.mask || a.mask[key]);
+    Own<T, D> kk, vv;
+    kk.load((const T *)a.K + (valid ? key : 0) * a.ld_k + (int64_t)kvh * a.d, seen, a.d, a.vec, h);
+    vv.load((const T *)a.V + (valid ? key : 0) * a.ld_v + (int64_t)kvh * a.d, seen, a.d, a.vec, h);
+
+    const int len = q.end - q.begin, tiles = (len + S::BR - 1) / S::BR, steps = tiles * a.group;
+    const int left = Mma<T>::left_offset(lane, L::STRIDE);
+    f32x16 dk[L::DT], dv[L::DT];
+#pragma unroll
+    for (int dt = 0; dt < L::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
+
+    Stage<T, D, S::BR, S::THREADS> qs, gs;
+    float lse = 0.f, delta = 0.f;
+    auto load = [&](int head, int t) {
+        qs.load((const T *)a.Q + q.begin * a.ld_q + (int64_t)head * a.d, a.ld_q, t * S::BR, len, a.d, a.vec, tid);
+        gs.load((const T *)a.dO + q.begin * a.ld_do + (int64_t)head * a.d, a.ld_do, t * S::BR, len, a.d, a.vec, tid);
+        if (tid < S::BR) {
+            const int row = t * S::BR + tid;
+            const int64_t at = (int64_t)(q.begin + row) * a.hq + head;
+            lse = row < len ? a.lse[at] : -INFINITY;
+            delta = row < len ? a.delta[at] : 0.f;
+        }
+    };
+    int head = kvh * a.group, t = 0;
+    if (steps) load(head, 0);
+    for (int step = 0; step < steps; ++step) {
+        char *qt = lds + (step & 1) * S::BUFFER, *gt = qt + S::TILE;
+        float *stat = (float *)(gt + S::TILE);
+        qs.store(qt, tid, nullptr);
+        gs.store(gt, tid, nullptr);
+        if (tid < S::BR) {
+            stat[tid] = lse == -INFINITY ? -INFINITY : -lse * LOG2E;    // no such row, or one that saw no key: p = 0
+            stat[S::BR + tid] = -delta;
+        }
+        __syncthreads();
+        if (++t == tiles) { t = 0; ++head; }
+        if (step + 1 < steps) load(head, t);
+#pragma unroll
+        for (int i = 0; i < S::NT; ++i) {
+            f32x16 p = product<T, D>(qt + 32 * i * L::STRIDE, kk, lane, f32x16{});
+            f32x16 g;
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x4 x = *(const f32x4 *)(stat + 32 * i + reg_row(r) + 4 * h);
+                const f32x4 y = *(const f32x4 *)(stat + S::BR + 32 * i + reg_row(r) + 4 * h);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    p[r + j] = exp2_fast(__builtin_fmaf(p[r + j], a.c, x[j]));
+                    g[r + j] = y[j];
+                }
+            }
+            g = product<T, D>(gt + 32 * i * L::STRIDE, vv, lane, g);
+            fold<T, D>(gt + 32 * i * L::STRIDE, p, left, dv);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] *= p[r];
+            fold<T, D>(qt + 32 * i * L::STRIDE, g, left, dk);
+        }
+    }
+    if (!valid) return;
+    if (!seen)                                          // a key that is left out: zero, whatever its lane added up
+#pragma unroll
+        for (int dt = 0; dt < L::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
+    store_row<T>((T *)a.dK + key * a.ld_dk + (int64_t)kvh * a.d, dk, a.scale, a.d, a.vec, h);
+    store_row<T>((T *)a.dV + key * a.ld_dv + (int64_t)kvh * a.d, dv, 1.f, a.d, a.vec, h);
+}
+
+}  // namespace attn
+}  // namespace hch

@@ -1,0 +1,97 @@
+// Launches of the attention kernels: the choice of an instance by element type and head width.  The instances of a type
+// are compiled in a source of their own (attn_bf16.hip, attn_f32.hip).
+#pragma once
+#include "api_common.hpp"
+#include "attn.hip.hpp"
+
+namespace hch {
+namespace attn {
+
+// `few`: the form for few query rows per shape (Keys<T, D, 1>).  flops: of the whole pass, for the profile.
+template <typename T> hch_status launch_fwd(const Args &a, bool few, double bytes, double flops, hipStream_t s);
+template <typename T> hch_status launch_bwd_dq(const Args &a, bool few, double bytes, double flops, hipStream_t s);
+template <typename T> hch_status launch_bwd_dkv(const Args &a, double bytes, double flops, hipStream_t s);
+
+#ifdef HCH_ATTN_TYPE
+template <typename F> void with_width(int d, F &&f)
+{
+    if (d <= 32) f(std::integral_constant<int, 32>{});
+    else if (d <= 64) f(std::integral_constant<int, 64>{});
+    else if (d <= 96) f(std::integral_constant<int, 96>{});
+    else f(std::integral_constant<int, 128>{});
+}
+
+template <typename T> hch_status launch_fwd(const Args &a, bool few, double bytes, double flops, hipStream_t s)
+{
+    {
+        LaunchTimer lt(HCH_KERNEL_ID("attn_fwd_kernel"), s, bytes, flops);
+        with_width(a.d, [&](auto w) {
+            constexpr int D = decltype(w)::value;
+            if (few) {
+                constexpr auto kernel = attn_fwd_kernel<T, D, 1>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(Keys<T, D, 1>::THREADS), 0, s, a);
+            } else {
+                constexpr auto kernel = attn_fwd_kernel<T, D, 4>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(Keys<T, D, 4>::THREADS), 0, s, a);
+            }
+        });
+    }
+    HCH_LAUNCH_CHECK("attn_fwd_kernel");
+    if (a.splits > 1) {
+        {
+            LaunchTimer lt(HCH_KERNEL_ID("attn_join_kernel"), s, (double)a.splits * a.nq * a.hq * (4 * a.d + 8), 0.0);
+            constexpr auto kernel = attn_join_kernel<T>;
+            HCH_LAUNCH(kernel, dim3((unsigned)(a.nq * a.hq)), dim3(256), 0, s, a);
+        }
+        HCH_LAUNCH_CHECK("attn_join_kernel");
+    }
+    return HCH_OK;
+}
+
+template <typename T> hch_status launch_bwd_dq(const Args &a, bool few, double bytes, double flops, hipStream_t s)
+{
+    {
+        LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_dq_kernel"), s, bytes, flops);
+        with_width(a.d, [&](auto w) {
+            constexpr int D = decltype(w)::value;
+            if (few) {
+                constexpr auto kernel = attn_bwd_dq_kernel<T, D, 1>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(Keys<T, D, 1>::THREADS), 0, s, a);
+            } else {
+                constexpr auto kernel = attn_bwd_dq_kernel<T, D, 4>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(Keys<T, D, 4>::THREADS), 0, s, a);
+            }
+        });
+    }
+    HCH_LAUNCH_CHECK("attn_bwd_dq_kernel");
+    if (a.splits > 1) {
+        {
+            LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_join_kernel"), s, (double)a.splits * a.nq * a.hq * 4 * a.d, 0.0);
+            constexpr auto kernel = attn_bwd_join_kernel<T>;
+            HCH_LAUNCH(kernel, dim3((unsigned)((a.nq * a.hq * a.d + 255) / 256)), dim3(256), 0, s, a);
+        }
+        HCH_LAUNCH_CHECK("attn_bwd_join_kernel");
+    }
+    return HCH_OK;
+}
+
+template <typename T> hch_status launch_bwd_dkv(const Args &a, double bytes, double flops, hipStream_t s)
+{
+    {
+        LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_dkv_kernel"), s, bytes, flops);
+        with_width(a.d, [&](auto w) {
+            constexpr auto kernel = attn_bwd_dkv_kernel<T, decltype(w)::value>;
+            HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(256), 0, s, a);
+        });
+    }
+    HCH_LAUNCH_CHECK("attn_bwd_dkv_kernel");
+    return HCH_OK;
+}
+
+template hch_status launch_fwd<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
+template hch_status launch_bwd_dq<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
+template hch_status launch_bwd_dkv<HCH_ATTN_TYPE>(const Args &, double, double, hipStream_t);
+#endif
+
+}  // namespace attn
+}  // namespace hch

@@ -1,8 +1,5 @@
 // C ABI of the hch library: host logic, table upload and kernel launches.
-#include "../../include/hch.h"
-
-#include <hip/hip_runtime.h>
-#include <hip/hip_ext.h>
+#include "api_common.hpp"
 
 #include <algorithm>
 #include <atomic>
@@ -27,28 +24,9 @@
 #include "conv_bf16.hip.hpp"
 #include "psh_device.hip.hpp"
 #include "occupancy.hip.hpp"
-#include "profile.hpp"
 #include "psh_build.hpp"
 
-// Every kernel launch of the library: carries the two timing events of the enclosing LaunchTimer,
-// if there is one and timing is on; an ordinary launch otherwise.
-#define HCH_LAUNCH(kernel, grid, block, lds, stream, ...)                                          \
-    do {                                                                                           \
-        hipEvent_t ev_a_ = hch::tls_start_event, ev_b_ = hch::tls_stop_event;                      \
-        hch::tls_start_event = hch::tls_stop_event = nullptr;                                      \
-        if (ev_a_) hipExtLaunchKernelGGL(kernel, grid, block, lds, stream, ev_a_, ev_b_, 0, __VA_ARGS__); \
-        else hipLaunchKernelGGL(kernel, grid, block, lds, stream, __VA_ARGS__);                    \
-    } while (0)
-
 namespace {
-
-thread_local std::string g_err;
-
-hch_status fail(hch_status st, const std::string &msg)
-{
-    g_err = msg;
-    return st;
-}
 
 // Every allocation of the library on the device.  The runtime keeps a failed one as its last error over later calls that
 // succeed; taken back here, or the next HCH_LAUNCH_CHECK, of this call or of another one, would report it as its own.
@@ -64,13 +42,6 @@ hipError_t device_malloc(void **p, size_t bytes)
         hipError_t e_ = (call);                                                            \
         if (e_ != hipSuccess)                                                              \
             return fail(HCH_EHIP, std::string(#call) + ": " + hipGetErrorString(e_));      \
-    } while (0)
-
-#define HCH_LAUNCH_CHECK(name)                                                             \
-    do {                                                                                   \
-        hipError_t e_ = hipGetLastError();                                                 \
-        if (e_ != hipSuccess)                                                              \
-            return fail(HCH_EHIP, std::string("launch ") + name + ": " + hipGetErrorString(e_)); \
     } while (0)
 
 // One level of the super-PSH, host and device side.
@@ -252,7 +223,7 @@ struct hch_levels {
     HostBlock host_block, host_phi;            // its host copies: positions, H*, T*, V*; offset tables
 };
 
-extern "C" const char *hch_last_error(void) { return g_err.c_str(); }
+extern "C" const char *hch_last_error(void) { return hch::tls_error.c_str(); }
 
 extern "C" void hch_free_levels(hch_levels *levels)
 {

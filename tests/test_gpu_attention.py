@@ -1,0 +1,303 @@
+"""hch_attn_fwd / hch_attn_bwd against the 64-bit oracle: head widths, shared heads, ragged and empty shapes, masks,
+strides, few queries against many keys, streams, graphs, refusals.
+
+The bounds follow from the arithmetic.  A score is a sum of d products in fp32, so it is off by E <= (d + 32) 2^-24
+times the sum of its terms' sizes (plus the rounding of the exponent's argument), a probability by the factor exp(2 E);
+sums of n terms in fp32 add n 2^-24 of the sum of the terms' sizes.  With bf16, probabilities and dS are rounded to 8
+bits before the second product (2^-8 of each term), O is (which the backward pass reads: D is off by
+2^-8 |dO|.|o|), and so is the result."""
+import numpy as np
+import pytest
+
+from oracle import block as K
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+hch = pytest.importorskip("paper_1803_11385_amd")
+
+TYPES = {"f32": (hch.HCH_F32, torch.float32), "bf16": (hch.HCH_BF16, torch.bfloat16)}
+U, EPS = 2.0 ** -24, 2.0 ** -8
+
+
+def _ws(nbytes):
+    t = torch.empty(int(nbytes) + 256, dtype=torch.uint8, device="cuda")
+    off = (-t.data_ptr()) % 256
+    return t[off: off + int(nbytes)]
+
+
+def _offsets(lens):
+    return np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+
+
+def _columns(x, dt, pad, shift):
+    """x as columns of a wider tensor whose other elements are NaN; `shift` columns in front."""
+    t = torch.full((x.shape[0], x.shape[1] + pad + shift), float("nan"), dtype=dt, device="cuda")
+    v = t[:, shift: shift + x.shape[1]]
+    v.copy_(torch.from_numpy(x).to(dt))
+    return t, v
+
+
+class Case:
+    """Inputs rounded to the type, the library's results and the oracle's."""
+
+    def __init__(self, dtype, lq, lk, hq, hkv, d, masked=0.0, pad=0, shift=0, gain=1.0, seed=0, backward=True, junk=False):
+        rng = np.random.default_rng(seed)
+        self.code, self.dt = TYPES[dtype]
+        self.bf16 = dtype == "bf16"
+        self.qo, self.ko = _offsets(lq), _offsets(lk)
+        nq, nk = int(self.qo[-1]), int(self.ko[-1])
+        self.dims = (hq, hkv, d)
+        self.scale = float(np.float32(d ** -0.5))
+        self.mask = None
+        if masked:
+            self.mask = rng.random(nk) >= masked
+            full = [b for b in range(len(lk)) if lk[b]]
+            if len(full) > 1:
+                self.mask[self.ko[full[1]]: self.ko[full[1] + 1]] = False
+        on = lambda a: torch.from_numpy(a.astype(np.float32)).to(self.dt).float().numpy()
+        q, k = on(gain * rng.normal(size=(nq, hq * d))), on(rng.normal(size=(nk, hkv * d)) + 0.5 * rng.normal(size=(1, hkv * d)))
+        v, do = on(rng.normal(size=(nk, hkv * d))), on(rng.normal(size=(nq, hq * d)))
+        self.host = dict(q=q, k=k, v=v, do=do)
+        self.t, self.whole = {}, {}
+        for name, x in self.host.items():
+            self.whole[name], self.t[name] = _columns(x, self.dt, pad, shift)
+        if junk and self.mask is not None:                      # what is left out may hold anything
+            out = torch.from_numpy(~self.mask).cuda()
+            self.t["k"][out] = float("nan")
+            self.t["v"][out] = float("inf")
+        empty = lambda n, h: _columns(np.full((n, h * d), np.nan, np.float32), self.dt, pad, shift)
+        for name, n, h in (("o", nq, hq), ("dq", nq, hq), ("dk", nk, hkv), ("dv", nk, hkv)):
+            self.whole[name], self.t[name] = empty(n, h)
+        self.lse = torch.full((nq, hq), float("nan"), device="cuda")
+        self.dqo, self.dko = torch.from_numpy(self.qo).cuda(), torch.from_numpy(self.ko).cuda()
+        self.dmask = None if self.mask is None else torch.from_numpy(self.mask.astype(np.uint8) * 3).cuda()
+        kinds = [hch.HCH_WS_FWD] + ([hch.HCH_WS_BWD_DATA] if backward else [])
+        self.ws = _ws(max(hch.hch_attn_workspace_bytes(x, self.code, len(lq), nq, nk, hq, hkv, d) for x in kinds))
+        self.ws.fill_(255)                                      # NaN, should anything be read that was not written
+        self.backward = backward
+        self.want = K.attention(q, k, v, self.qo, self.ko, self.mask, hq, hkv, d, self.scale, do if backward else None)
+
+    def run(self, stream=None, lse=True):
+        t, (hq, hkv, d) = self.t, self.dims
+        hch.hch_attn_fwd(self.code, t["q"], t["k"], t["v"], t["o"], self.lse if lse else None, self.dqo, self.dko, self.dmask,
+                         hq, hkv, d, self.scale, self.ws, stream=stream)
+        if self.backward:
+            hch.hch_attn_bwd(self.code, t["q"], t["k"], t["v"], t["o"], self.lse, t["do"], t["dq"], t["dk"], t["dv"], self.dqo,
+                             self.dko, self.dmask, hq, hkv, d, self.scale, self.ws, stream=stream)
+        return self
+
+    def bounds(self):
+        w, (hq, hkv, d) = self.want, self.dims
+        n = int(np.diff(self.ko).max(initial=0))
+        nq = int(np.diff(self.qo).max(initial=0)) * (hq // hkv)
+        e = (d + 32) * U * w["top"] + 8 * U * (1 + np.log(max(n, 1)))
+        b = EPS if self.bf16 else 0.0
+        r = dict(o=(2 * e + (n + 16) * U + b) * w["o_abs"] + b * abs(w["o"]))
+        r["lse"] = np.where(np.isneginf(w["lse"]), 0.0, e + (n + 16) * U + 4 * U * abs(np.where(np.isneginf(w["lse"]), 0, w["lse"])))
+        if self.backward:
+            r["dv"] = (2 * e + (nq + 16) * U + b) * w["dv_abs"] + b * abs(w["dv"])
+            r["dq"] = (2 * e + (n + d + 16) * U + b) * w["dq_abs"] + b * w["d_abs"] * w["pk_abs"] + b * abs(w["dq"])
+            r["dk"] = (2 * e + (nq + d + 16) * U + b) * w["dk_abs"] + b * w["dk_d"] + b * abs(w["dk"])
+        return r
+
+    def check(self, lse=True):
+        torch.cuda.synchronize()
+        for name, bound in self.bounds().items():
+            if name == "lse" and not lse:
+                continue
+            got = (self.lse if name == "lse" else self.t[name]).double().cpu().numpy()
+            want = self.want[name]
+            if name == "lse":
+                assert np.array_equal(np.isneginf(got), np.isneginf(want)), "lse: rows without a key"
+                got, want = np.where(np.isneginf(want), 0, got), np.where(np.isneginf(want), 0, want)
+            assert not np.isnan(got).any(), f"{name}: NaN at {np.argwhere(np.isnan(got))[:4].tolist()}"
+            off = np.abs(got - want) - bound - 1e-30
+            assert (off <= 0).all(), f"{name}: {int((off > 0).sum())} of {off.size} beyond the bound, worst {off.max()}"
+        for name, v in self.t.items():                          # nothing beside the columns was touched
+            w = self.whole[name]
+            left = (v.data_ptr() - w.data_ptr()) // w.element_size()
+            assert torch.isnan(w[:, :left]).all() and torch.isnan(w[:, left + v.shape[1]:]).all(), name
+        return self
+
+
+RAGGED = [1, 2, 31, 0, 32, 33, 64, 65, 127, 128, 129, 190]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 32), (4, 2, 64), (3, 1, 96), (2, 1, 128), (2, 2, 16), (3, 1, 40), (2, 2, 1), (2, 1, 20),
+                                      (1, 1, 33), (4, 4, 120)])
+def test_ragged_shapes_against_the_oracle(dtype, hq, hkv, d):
+    Case(dtype, RAGGED, RAGGED, hq, hkv, d, seed=d).run().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [24, 64, 128])
+def test_masks_and_what_they_leave_out(dtype, d):
+    """A quarter of the keys and all keys of one shape left out; K and V hold NaN and infinity there."""
+    Case(dtype, [3, 70, 140, 1], [130, 65, 200, 1], 4, 2, d, masked=0.25, junk=True, seed=d).run().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift", [(64, 0), (8, 8), (3, 0), (0, 1), (2, 5)])
+def test_rows_that_are_part_of_wider_rows(dtype, pad, shift):
+    Case(dtype, [40, 9, 77], [33, 140, 5], 4, 2, 32, masked=0.3, pad=pad, shift=shift, seed=pad).run().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lq,lk,hq,hkv,d", [([1], [1], 1, 1, 64), ([1, 1, 1], [1, 700, 3000], 4, 4, 16), ([1], [9000], 8, 2, 32),
+                                            ([3, 0, 2], [0, 400, 2500], 4, 1, 96), ([5, 7], [1025, 4096], 2, 1, 128),
+                                            ([16], [5000], 2, 1, 24), ([300], [7], 2, 2, 64), ([0, 2], [50, 60], 2, 2, 32)])
+def test_few_queries_against_many_keys(dtype, lq, lk, hq, hkv, d):
+    Case(dtype, lq, lk, hq, hkv, d, masked=0.2 if len(lk) > 2 else 0.0, seed=sum(lk)).run().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_queries_whose_keys_are_split(dtype):
+    Case(dtype, [130], [2100], 1, 1, 64, seed=5).run().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gain", [0.0, 30.0])
+def test_flat_and_peaked_rows(dtype, gain):
+    Case(dtype, [50, 20], [150, 300], 2, 2, 64, gain=gain, seed=3).run().check()
+
+
+def test_many_small_shapes():
+    rng = np.random.default_rng(1)
+    lq, lk = rng.integers(0, 4, 5000), rng.integers(0, 5, 5000)
+    Case("f32", lq, lk, 2, 1, 16, masked=0.1, seed=1).run().check()
+    Case("bf16", rng.integers(0, 70, 300), rng.integers(0, 70, 300), 1, 1, 32, seed=2).run().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nothing_to_do(dtype):
+    c = Case(dtype, [0, 0], [5, 9], 2, 2, 32).run()
+    torch.cuda.synchronize()
+    assert not c.t["dk"].any() and not c.t["dv"].any()
+    c = Case(dtype, [5, 9], [0, 0], 2, 2, 32).run()
+    torch.cuda.synchronize()
+    assert not c.t["o"].any() and not c.t["dq"].any() and torch.isneginf(c.lse).all()
+    Case(dtype, [0], [0], 2, 2, 32).run()
+    Case(dtype, [], [], 2, 2, 32).run()
+    c = Case(dtype, [40], [50], 2, 1, 64, backward=False).run(lse=False).check(lse=False)
+    assert torch.isnan(c.lse).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_gradient_row_without_keys_is_zero_whatever_it_holds(dtype):
+    c = Case(dtype, [4, 3], [40, 50], 2, 2, 32, masked=0.1)      # the second shape sees nothing
+    c.t["do"][4:] = float("nan")
+    c.run()
+    torch.cuda.synchronize()
+    assert not c.t["dq"][4:].any() and not c.t["dk"][40:].any() and not c.t["dv"][40:].any()
+    assert not torch.isnan(c.t["dk"]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lq,lk", [([200, 90], [200, 90]), ([1, 1], [5000, 700])])
+def test_same_bits_again_on_another_stream_and_in_a_graph(dtype, lq, lk):
+    c = Case(dtype, lq, lk, 4, 2, 64, masked=0.1, seed=9).run().check()
+    names = ("o", "dq", "dk", "dv")
+    first = [c.t[n].clone() for n in names] + [c.lse.clone()]
+
+    def same(what):
+        torch.cuda.synchronize()
+        for a, b in zip(first, [c.t[n] for n in names] + [c.lse]):
+            assert torch.equal(a, b), what
+
+    def wipe():
+        for n in names:
+            c.t[n].fill_(7.0)
+
+    wipe()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    c.run(stream=s.cuda_stream)
+    same("another stream")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.run()
+    for _ in range(3):
+        wipe()
+        c.ws.fill_(255)
+        g.replay()
+        same("replay")
+
+
+def test_gradient_is_the_difference_of_the_outputs():
+    """Along a random direction, from the library's own forward passes: the second-order term and fp32's noise stay
+    under 1e-3 of the sizes involved at a step of 1/64."""
+    h = 1.0 / 64
+    base = Case("f32", [60, 33], [90, 120], 4, 2, 32, masked=0.1, seed=21).run()
+    torch.cuda.synchronize()
+    rng = np.random.default_rng(4)
+    for name, grad in (("q", "dq"), ("k", "dk"), ("v", "dv")):
+        u = torch.from_numpy(rng.normal(size=base.host[name].shape).astype(np.float32)).cuda()
+        u /= u.norm()
+        x = base.t[name].clone()
+        side = []
+        for s in (h, -h):
+            base.t[name].copy_(x + s * u)
+            hch.hch_attn_fwd(base.code, base.t["q"], base.t["k"], base.t["v"], base.t["o"], None, base.dqo, base.dko, base.dmask,
+                             *base.dims, base.scale, base.ws)
+            side.append((base.t["o"].double() * base.t["do"].double()).sum().item())
+        base.t[name].copy_(x)
+        want = (base.t[grad].double() * u.double()).sum().item()
+        assert abs((side[0] - side[1]) / (2 * h) - want) < 1e-3 * (1 + base.t[grad].norm().item())
+
+
+def test_offsets_beyond_32_bits():
+    """Keys whose elements lie more than 2^31 elements behind the first."""
+    n, ld, d = 560000, 4000, 32
+    big = torch.zeros((n, ld), dtype=torch.bfloat16, device="cuda")
+    assert big.numel() > 2 ** 31
+    rng = np.random.default_rng(0)
+    k, v, q = (torch.from_numpy(rng.normal(size=(300 if i < 2 else 2, d)).astype(np.float32)).bfloat16() for i in range(3))
+    big[-300:, :d], big[-300:, d: 2 * d] = k.cuda(), v.cuda()
+    qo, ko = torch.tensor([0, 1, 2], dtype=torch.int32).cuda(), torch.tensor([0, n - 300, n], dtype=torch.int32).cuda()
+    o, lse = torch.empty((2, d), dtype=torch.bfloat16, device="cuda"), torch.empty((2, 1), device="cuda")
+    ws = _ws(max(hch.hch_attn_workspace_bytes(x, hch.HCH_BF16, 2, 2, n, 1, 1, d) for x in (hch.HCH_WS_FWD, hch.HCH_WS_BWD_DATA)))
+    hch.hch_attn_fwd(hch.HCH_BF16, q.cuda(), big[:, :d], big[:, d: 2 * d], o, lse, qo, ko, None, 1, 1, d, d ** -0.5, ws)
+    w = K.attention(q[1:].float().numpy(), k.float().numpy(), v.float().numpy(), [0, 1], [0, 300], None, 1, 1, d, d ** -0.5,
+                    np.ones((1, d)))
+    torch.cuda.synchronize()
+    assert (np.abs(o[1].double().cpu().numpy() - w["o"][0]) <= 2.01 * EPS * w["o_abs"][0]).all() and not o[0].any()
+    # and the gradients, written into the same rows
+    dq, do = torch.empty_like(o), torch.ones((2, d), dtype=torch.bfloat16, device="cuda")
+    hch.hch_attn_bwd(hch.HCH_BF16, q.cuda(), big[:, :d], big[:, d: 2 * d], o, lse, do, dq, big[:, 2 * d: 3 * d], big[:, 3 * d: 4 * d],
+                     qo, ko, None, 1, 1, d, d ** -0.5, ws)
+    torch.cuda.synchronize()
+    got = big[-300:, 3 * d: 4 * d].double().cpu().numpy()
+    assert (np.abs(got - w["dv"]) <= 2.01 * EPS * w["dv_abs"]).all()
+    assert not big[:, 4 * d:].any()
+
+
+def test_refusals():
+    c = Case("f32", [4], [6], 2, 1, 32)
+    t = c.t
+
+    def status(**kw):
+        a = dict(code=c.code, q=t["q"], k=t["k"], v=t["v"], o=t["o"], lse=c.lse, qo=c.dqo, ko=c.dko, mask=None, hq=2, hkv=1, d=32,
+                 scale=1.0, ws=c.ws)
+        a.update(kw)
+        with pytest.raises(hch.HchError) as e:
+            hch.hch_attn_fwd(a["code"], a["q"], a["k"], a["v"], a["o"], a["lse"], a["qo"], a["ko"], a["mask"], a["hq"], a["hkv"],
+                             a["d"], a["scale"], a["ws"])
+        return e.value.status
+
+    assert status(code=5) == 1 and status(code=hch.HCH_BF16) == 1
+    assert status(hkv=3) == 1 and status(hq=0) == 1 and status(d=0) == 1 and status(d=64) == 1
+    assert status(scale=0.0) == 1 and status(scale=float("nan")) == 1 and status(scale=float("inf")) == 1
+    assert status(q=t["q"].cpu()) == 1 and status(v=t["v"][:5]) == 1 and status(k=t["k"].t()) == 1
+    assert status(q=t["q"].reshape(-1)) == 1 and status(o=t["o"].expand(4, 64)[:1].expand(4, 64)) == 1
+    assert status(lse=c.lse[:2]) == 1 and status(mask=torch.ones(6, device="cuda")) == 1
+    assert status(mask=torch.ones(5, dtype=torch.uint8, device="cuda")) == 1
+    assert status(qo=c.dqo.long()) == 1 and status(ko=c.dko[:1]) == 1 and status(qo=c.dqo.cpu()) == 1
+    assert status(ws=c.ws[:0]) in (1, 6) and status(ws=c.ws[:128]) == 6 and status(ws=c.ws[1:]) == 1
+    wide = torch.zeros((4, 2 * 160), device="cuda")
+    assert status(q=wide, o=wide, d=160, hkv=2, k=torch.zeros((6, 320), device="cuda"), v=torch.zeros((6, 320), device="cuda")) == 5
+    assert hch.hch_attn_workspace_bytes(hch.HCH_WS_BWD_WEIGHT, c.code, 1, 4, 6, 2, 1, 32) == 0
+    assert hch.hch_attn_workspace_bytes(hch.HCH_WS_FWD, c.code, 1, 4, 6, 2, 3, 32) == 0
+    assert hch.hch_attn_workspace_bytes(hch.HCH_WS_FWD, c.code, 0, 4, 6, 2, 2, 32) == 0
+    c.run().check()                                             # and a call after them is none the worse

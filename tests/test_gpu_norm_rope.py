@@ -1,0 +1,220 @@
+"""hch_layernorm_* and hch_rope_* against the 64-bit oracle.
+
+Bounds: sums over c channels in fp32 are off by c 2^-24 of the sum of their terms' sizes at most; the variance's
+relative error 2^-23 (c + 8) reaches y with half of it.  A turned pair is off by 2^-22 of its length.  Results in bf16 are
+rounded once: 2^-8."""
+import numpy as np
+import pytest
+
+from oracle import block as K
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+hch = pytest.importorskip("paper_1803_11385_amd")
+
+TYPES = {"f32": (hch.HCH_F32, torch.float32), "bf16": (hch.HCH_BF16, torch.bfloat16)}
+U = 2.0 ** -24
+ROUND = {"f32": 2.0 ** -23, "bf16": 2.0 ** -8}
+
+
+def _ws(nbytes):
+    t = torch.full((int(nbytes) + 256,), 255, dtype=torch.uint8, device="cuda")
+    off = (-t.data_ptr()) % 256
+    return t[off: off + int(nbytes)]
+
+
+def _on(rng, shape, dtype, shift=0.0):
+    x = torch.from_numpy((rng.normal(size=shape) + shift).astype(np.float32)).to(TYPES[dtype][1])
+    return x.cuda(), x.double().numpy()
+
+
+def _near(got, want, bound, what):
+    torch.cuda.synchronize()
+    off = np.abs(got.double().cpu().numpy() - want) - bound
+    assert (off <= 0).all(), f"{what}: {int((off > 0).sum())} of {off.size} beyond the bound, worst {off.max()}"
+
+
+CHANNELS = [1, 2, 3, 4, 16, 17, 32, 50, 64, 100, 128, 200, 256, 260, 512, 515, 1000, 1024, 2048, 2050, 4096, 8192]
+
+
+@pytest.mark.parametrize("x,y", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("c", CHANNELS)
+def test_layernorm_and_gradients(x, y, c):
+    rng = np.random.default_rng(c)
+    for n, residual, affine in ((1, False, True), (37, True, True), (1030 if c <= 256 else 70, True, False)):
+        X, xs = _on(rng, (n, c), x, 3.0)
+        R, rs_ = _on(rng, (n, c), x) if residual else (None, None)
+        g, gs = _on(rng, (c,), "f32", 1.0) if affine else (None, None)
+        b, bs = _on(rng, (c,), "f32") if affine else (None, None)
+        S = torch.empty_like(X) if residual else None
+        Y = torch.empty((n, c), dtype=TYPES[y][1], device="cuda")
+        stats = torch.empty((n, 2), device="cuda")
+        eps = 1e-5
+        hch.hch_layernorm_fwd(TYPES[x][0], X, R, S, g, b, TYPES[y][0], Y, stats, n, c, eps)
+        s, want, wstats = K.layernorm_fwd(xs, rs_, gs, bs, eps)
+        size = np.abs(s).max(1, keepdims=True)
+        if residual:
+            _near(S, s, ROUND[x] * np.abs(s), "s")
+        # the mean's error, then the relative one of the deviation
+        dev = wstats[:, 1:]
+        ga, ba = (np.abs(gs) if affine else 1.0), (np.abs(bs) if affine else 0.0)
+        h = np.abs((s - wstats[:, :1]) * dev)
+        dmean = (c + 4) * U * size
+        rel = (c + 16) * 2 * U + dmean ** 2 * dev ** 2 + 2 * dmean * dev * h.mean(1, keepdims=True)
+        bound = (dmean * dev * (1 + rel) + rel * h) * ga + 8 * U * (h * ga + ba) + ROUND[y] * np.abs(want)
+        _near(Y, want, bound + 1e-30, "y")
+        _near(stats[:, :1], wstats[:, :1], dmean + 1e-30, "mean")
+        _near(stats[:, 1:], dev, rel * dev + 1e-30, "1 / deviation")
+
+        DY, dys = _on(rng, (n, c), y)
+        DS, dss = _on(rng, (n, c), x) if residual else (None, None)
+        src, srcs = (S, S.double().cpu().numpy()) if residual else (X, xs)
+        dX = torch.empty_like(X)
+        dg, db = torch.full((c,), float("nan"), device="cuda"), torch.full((c,), float("nan"), device="cuda")
+        ws = _ws(hch.hch_layernorm_workspace_bytes(n, c))
+        hch.hch_layernorm_bwd(TYPES[x][0], src, stats, g, TYPES[y][0], DY, DS, dX, dg, db, n, c, ws)
+        st = stats.double().cpu().numpy()
+        wdx, wdg, wdb = K.layernorm_bwd(srcs, st, gs, dys, dss)
+        h = (np.abs(srcs) + np.abs(st[:, :1])) * st[:, 1:]      # sizes of what the differences are taken of
+        w = np.abs(dys) * ga
+        terms = st[:, 1:] * (w + w.mean(1, keepdims=True) + h * (w * h).mean(1, keepdims=True))
+        bound = (c + 16) * 2 * U * terms + 4 * U * np.abs(wdx) + ROUND[x] * np.abs(wdx) + (U * np.abs(dss) if residual else 0)
+        _near(dX, wdx, bound + 1e-30, "dx")
+        _near(dg, wdg, (n + 16) * U * (np.abs(dys) * h).sum(0) + 1e-30, "dgamma")
+        _near(db, wdb, (n + 16) * U * np.abs(dys).sum(0) + 1e-30, "dbeta")
+        # the same bits again, and without the weights' gradient
+        dX2, dg2, db2 = torch.empty_like(dX), torch.empty_like(dg), torch.empty_like(db)
+        hch.hch_layernorm_bwd(TYPES[x][0], src, stats, g, TYPES[y][0], DY, DS, dX2, dg2, db2, n, c, ws)
+        assert torch.equal(dX, dX2) and torch.equal(dg, dg2) and torch.equal(db, db2)
+        dX2.zero_()
+        hch.hch_layernorm_bwd(TYPES[x][0], src, stats, g, TYPES[y][0], DY, DS, dX2, None, None, n, c, None)
+        assert torch.equal(dX, dX2)
+
+
+@pytest.mark.parametrize("c", [7, 64])
+def test_layernorm_in_place_unaligned_and_large_means(c):
+    rng = np.random.default_rng(c)
+    n = 333
+    flat = torch.zeros(n * c + 1, device="cuda")
+    X = flat[1:].view(n, c)                                     # 4 bytes past a 16-byte boundary
+    xs = (rng.normal(size=(n, c)) + 1000.0).astype(np.float32)
+    X.copy_(torch.from_numpy(xs))
+    R, rs_ = _on(rng, (n, c), "f32")
+    Y = torch.empty((n, c), device="cuda")
+    hch.hch_layernorm_fwd(hch.HCH_F32, X, R, X, None, None, hch.HCH_F32, Y, None, n, c, 1e-5)     # S = X
+    s, want, st = K.layernorm_fwd(xs, rs_, None, None, 1e-5)
+    # the sum is rounded to fp32 at 1000: 2^-15 of a unit, against a deviation of about 1.4
+    _near(X, s, 2.0 ** -14 + 0 * s, "s")
+    _near(Y, want, ((c + 8) * U * 1100 + 2.0 ** -14) * st[:, 1:] * (1 + np.abs(want)), "y")
+    assert flat[0] == 0
+
+
+def test_layernorm_of_a_constant_row_and_of_nothing():
+    X = torch.full((5, 24), 2.5, device="cuda")
+    Y = torch.empty_like(X)
+    stats = torch.empty((5, 2), device="cuda")
+    hch.hch_layernorm_fwd(hch.HCH_F32, X, None, None, None, None, hch.HCH_F32, Y, stats, 5, 24, 1e-5)
+    torch.cuda.synchronize()
+    assert not Y.any() and (stats[:, 0] == 2.5).all() and torch.allclose(stats[:, 1], torch.tensor(1e5 ** 0.5).cuda())
+    dg, db = torch.ones(24, device="cuda"), torch.ones(24, device="cuda")
+    e = torch.empty((0, 24), device="cuda")
+    hch.hch_layernorm_fwd(hch.HCH_F32, X, None, None, None, None, hch.HCH_F32, Y, None, 0, 24)
+    hch.hch_layernorm_bwd(hch.HCH_F32, X, stats, None, hch.HCH_F32, X, None, X, dg, db, 0, 24, _ws(hch.hch_layernorm_workspace_bytes(0, 24)))
+    torch.cuda.synchronize()
+    assert not dg.any() and not db.any() and e.numel() == 0
+
+
+def test_layernorm_row_with_nan_spoils_no_other():
+    X = torch.randn((40, 20), device="cuda")
+    X[3, 5], X[17, 0] = float("nan"), float("inf")
+    Y = torch.empty_like(X)
+    hch.hch_layernorm_fwd(hch.HCH_F32, X, None, None, None, None, hch.HCH_F32, Y, None, 40, 20)
+    bad = torch.isnan(Y).any(1)
+    torch.cuda.synchronize()
+    assert bad.nonzero().flatten().tolist() == [3, 17]
+
+
+@pytest.mark.parametrize("x,y", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("n,heads,rot,d,sections,pad", [(1, 1, 1, 2, (1, 0, 0), 0), (300, 12, 8, 64, (11, 11, 10), 0),
+                                                        (77, 3, 2, 32, (5, 5, 5), 6), (50, 4, 4, 6, (1, 1, 1), 3), (9, 2, 0, 8, (0, 0, 0), 0),
+                                                        (33, 5, 5, 256, (43, 43, 42), 0), (2000, 3, 3, 128, (20, 22, 22), 128), (65, 1, 1, 20, (0, 7, 1), 4)])
+def test_rope_and_its_way_back(x, y, n, heads, rot, d, sections, pad):
+    rng = np.random.default_rng(n)
+    pos = rng.integers(-3, 600, size=(n, 3)).astype(np.int32)
+    if n > 4:
+        pos[1], pos[2] = (32767, 32000, 31001), (2 ** 30, -2 ** 31, 2 ** 31 - 1)
+    wide, xs = _on(rng, (n, heads * d + pad), x)
+    X, xs = wide[:, pad:], xs[:, pad:]
+    P = torch.from_numpy(pos).cuda()
+    for inverse, f in ((False, hch.hch_rope_fwd), (True, hch.hch_rope_bwd)):
+        out = torch.full((n, heads * d + pad), float("nan"), dtype=TYPES[y][1], device="cuda")
+        Y = out[:, pad:]
+        f(TYPES[x][0], X, TYPES[y][0], Y, P, n, heads, rot, d, sections, 10000.0, 0.5)
+        want = K.rope(xs, pos, heads, rot, d, sections, 10000.0, 0.5, inverse)
+        z = xs.reshape(n, heads, d // 2, 2)
+        length = np.repeat(np.sqrt((z ** 2).sum(-1)), 2, axis=-1).reshape(n, heads * d)
+        # a coordinate of 2^31 leaves 2^-53 * 2^31 of a turn of error in 64 bits: nothing beside fp32's
+        _near(Y, want, 2.0 ** -21 * length + ROUND[y] * np.abs(want), "inverse" if inverse else "forward")
+        assert torch.isnan(out[:, :pad]).all()
+        kept = torch.from_numpy(xs[:, rot * d:]).cuda().to(TYPES[y][1])
+        assert torch.equal(Y[:, rot * d:], kept)                # heads that are not turned
+
+
+def test_rope_in_place_keeps_infinities_apart_and_level_positions():
+    import synth_shapes as S
+    coords, _ = S.sphere_shell_32()
+    lv = hch.hch_build_levels(coords, [0, coords.shape[0]], 32, 2)
+    pos, off = lv.device_positions(1), lv.device_offsets(1)
+    n = lv.n(1)
+    assert off.tolist() == [0, n] and np.array_equal(pos.cpu().numpy(), lv.info(1).device_coords())
+    X = torch.randn((n, 2 * 16), device="cuda")
+    X[0, 30], X[0, 31], X[1, 14] = float("inf"), float("nan"), float("inf")      # an unturned pair; the pair beyond the sections
+    want = torch.empty_like(X)
+    hch.hch_rope_fwd(hch.HCH_F32, X, hch.HCH_F32, want, pos, n, 2, 1, 16, (3, 2, 2))
+    hch.hch_rope_fwd(hch.HCH_F32, X, hch.HCH_F32, X, pos, n, 2, 1, 16, (3, 2, 2))
+    torch.cuda.synchronize()
+    assert torch.equal(torch.nan_to_num(X, 9.0), torch.nan_to_num(want, 9.0))
+    assert torch.isinf(X[0, 30]) and torch.isnan(X[0, 31]) and torch.isinf(X[1, 14]) and not torch.isnan(X[1]).any()
+
+
+def test_refusals():
+    X, s = torch.zeros((4, 8), device="cuda"), torch.zeros((4, 2), device="cuda")
+    g, p = torch.zeros(8, device="cuda"), torch.zeros((4, 3), dtype=torch.int32, device="cuda")
+    F = hch.HCH_F32
+
+    def status(f, *a):
+        with pytest.raises(hch.HchError) as e:
+            f(*a)
+        return e.value.status
+
+    fwd, bwd, rope = hch.hch_layernorm_fwd, hch.hch_layernorm_bwd, hch.hch_rope_fwd
+    assert status(fwd, 7, X, None, None, g, g, F, X, None, 4, 8) == 1
+    assert status(fwd, F, X, X, None, g, g, F, X, None, 4, 8) == 1             # R without S
+    assert status(fwd, F, X, None, None, g, g, F, X, None, 4, 0) == 1
+    assert status(fwd, F, X, None, None, g, g, F, X, None, -1, 8) == 1
+    assert status(fwd, F, X, None, None, g, g, F, X, None, 4, 8, -1.0) == 1
+    assert status(fwd, F, X, None, None, g, g, F, X, None, 5, 8) == 1          # shorter than the call reads
+    assert status(fwd, F, X.half(), None, None, g, g, F, X, None, 4, 8) == 1
+    assert status(fwd, F, X, None, None, g, g, F, None, None, 4, 8) == 1
+    big = torch.zeros(8193, device="cuda")
+    assert status(fwd, F, big, None, None, None, None, F, big, None, 1, 8193) == 5
+    assert hch.hch_layernorm_workspace_bytes(1, 8193) == 0 and hch.hch_layernorm_workspace_bytes(-1, 8) == 0
+    assert status(bwd, F, X, s, g, F, X, None, X, g, None, 4, 8, None) == 1
+    assert status(bwd, F, X, s, g, F, X, None, X, g, g, 4, 8, None) == 1
+    assert status(bwd, F, X, s, g, F, X, None, X, g, g, 4, 8, _ws(256)[:128]) == 6
+    assert status(bwd, F, X, None, g, F, X, None, X, g, g, 4, 8, _ws(512)) == 1
+    Y = torch.zeros((4, 8), device="cuda")
+    assert status(rope, F, X, F, Y, p, 4, 1, 1, 7, (1, 1, 1)) == 1             # odd width
+    assert status(rope, F, X, F, Y, p, 4, 2, 3, 4, (1, 1, 0)) == 1
+    assert status(rope, F, X, F, Y, p, 4, 1, 1, 8, (2, 2, 1)) == 1             # five pairs of four
+    assert status(rope, F, X, F, Y, p, 4, 1, 1, 8, (-1, 2, 1)) == 1
+    assert status(rope, F, X, F, Y, p, 4, 1, 1, 8, (1, 1)) == 1
+    assert status(rope, F, X, F, Y, p, 4, 2, 1, 8, (1, 1, 1)) == 1             # rows too short
+    assert status(rope, F, X, F, Y, p, 5, 1, 1, 8, (1, 1, 1)) == 1
+    assert status(rope, F, X, F, Y, None, 4, 1, 1, 8, (1, 1, 1)) == 1
+    assert status(rope, F, X, F, Y, p[:3], 4, 1, 1, 8, (1, 1, 1)) == 1
+    assert status(rope, F, X, F, Y, p, 4, 1, 1, 8, (1, 1, 1), -2.0) == 1
+    assert status(rope, F, X, F, Y, p, 4, 1, 1, 8, (1, 1, 1), 10.0, float("nan")) == 1
+    w = torch.zeros((4, 258), device="cuda")
+    assert status(rope, F, w, F, w.clone(), p, 4, 1, 1, 258, (1, 1, 1)) == 5
