@@ -324,11 +324,25 @@ class Levels:
             pass
 
 
-def _stream(stream):
-    if stream is None:
+_torch = None
+
+
+def _th():
+    """torch, imported by the first call that has a tensor to check."""
+    global _torch
+    if _torch is None:
         import torch
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
-    return C.c_void_p(int(stream))
+        _torch = torch
+    return _torch
+
+
+def _stream(stream):
+    """The stream's address; None: torch's current one (by its raw accessor where there is one: 0.1 us in place of 1)."""
+    if stream is not None:
+        return int(stream)
+    th = _torch or _th()
+    raw = getattr(th._C, "_cuda_getCurrentRawStream", None)
+    return raw(th.cuda.current_device()) if raw else th.cuda.current_stream().cuda_stream
 
 
 # Every DEVICE argument is checked here, on the host, before its address goes to the library: a
@@ -341,16 +355,16 @@ def _dp(t, what="tensor", kind=None, numel=0):
     """Address of a DEVICE tensor (None -> NULL).  kind: _F32, _I32, an hch_dtype (HCH_F32 / HCH_BF16:
     float32, or any 2-byte element type holding bfloat16 bit patterns), or None (bytes)."""
     if t is None:
-        return C.c_void_p(None)
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        return None
+    th = _torch or _th()
+    if not isinstance(t, th.Tensor) or not t.is_cuda:
         raise HchError(1, f"{what}: must be a torch tensor in GPU memory")
     if not t.is_contiguous():
         raise HchError(1, f"{what}: must be contiguous")
     if kind == _F32 or kind == HCH_F32:
-        ok = t.dtype == torch.float32
+        ok = t.dtype == th.float32
     elif kind == _I32:
-        ok = t.dtype == torch.int32
+        ok = t.dtype == th.int32
     elif kind == HCH_BF16:
         ok = t.element_size() == 2
     else:
@@ -359,7 +373,7 @@ def _dp(t, what="tensor", kind=None, numel=0):
         raise HchError(1, f"{what}: wrong element type {t.dtype}")
     if t.numel() < numel:
         raise HchError(1, f"{what}: {t.numel()} elements, the call needs {int(numel)}")
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _nbytes(ws):
@@ -690,16 +704,17 @@ def hch_layernorm_bwd(x_dtype, X, stats, gamma, dy_dtype, dY, dS, dX, dgamma, db
 
 def _rows(t, what, dtype, n, width):
     """Address and row stride of n rows of `width` elements: a 2-D tensor, or a part of the columns of one."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    th = _torch or _th()
+    if not isinstance(t, th.Tensor) or not t.is_cuda:
         raise HchError(1, f"{what}: must be a torch tensor in GPU memory")
-    if t.dtype != torch.float32 if dtype == HCH_F32 else t.element_size() != 2:
+    if t.dtype != th.float32 if dtype == HCH_F32 else t.element_size() != 2:
         raise HchError(1, f"{what}: wrong element type {t.dtype}")
-    if t.dim() != 2 or t.shape[0] < n or t.shape[1] < width:
-        raise HchError(1, f"{what}: needs {n} rows of {width} elements, has {tuple(t.shape)}")
-    ld, step = t.stride()
+    shape = t.shape
+    if len(shape) != 2 or shape[0] < n or shape[1] < width:
+        raise HchError(1, f"{what}: needs {n} rows of {width} elements, has {tuple(shape)}")
     if n == 0:
         return t.data_ptr(), width
+    ld, step = t.stride()
     if (step != 1 and width > 1) or (n > 1 and ld < width):
         raise HchError(1, f"{what}: the elements of a row must lie side by side and rows must not overlap")
     return t.data_ptr(), ld if n > 1 else max(ld, width)
@@ -733,50 +748,53 @@ def hch_attn_workspace_bytes(kind, dtype, batch, n_q, n_k, heads_q, heads_kv, he
     return int(load_library().hch_attn_workspace_bytes(C.byref(d), kind))
 
 
-def _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale, q_rows, k_rows):
-    """Description and addresses; q_rows / k_rows: names and tensors shaped like the queries / the keys, each of which
-    gives its stride to ld_<name>."""
-    import torch
+def _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale):
+    """Description of a call without its row strides, and the lengths of a query's and of a key's row."""
+    th = _torch or _th()
     dt = _in_dtype(dtype)
     for t, what in ((Q, "Q"), (K, "K")):
-        if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        if not isinstance(t, th.Tensor) or t.dim() != 2:
             raise HchError(1, f"{what}: must be a torch tensor of rows")
     n_q, n_k = Q.shape[0], K.shape[0]
-    batch = q_offsets.numel() - 1
-    if batch < 0 or k_offsets.numel() != q_offsets.numel():
+    qo, ko, mask = _dp(q_offsets, "q_offsets", _I32), _dp(k_offsets, "k_offsets", _I32), None
+    batch = q_offsets.numel() - 1 if qo is not None and ko is not None else -1
+    if batch < 0 or k_offsets.numel() != batch + 1:
         raise HchError(1, "q_offsets and k_offsets: batch + 1 entries each")
-    d = _AttnDesc(dtype=dt, batch=batch, heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim, scale=scale, n_q=n_q, n_k=n_k,
-                  q_offsets=_dp(q_offsets, "q_offsets", _I32).value, k_offsets=_dp(k_offsets, "k_offsets", _I32).value)
     if key_mask is not None:
         if key_mask.element_size() != 1:
             raise HchError(1, "key_mask: must have elements of one byte")
-        d.key_mask = _dp(key_mask, "key_mask", None, n_k).value
-    ptr = {}
-    for rows, n, w in ((q_rows, n_q, heads_q * head_dim), (k_rows, n_k, heads_kv * head_dim)):
-        for name, t in rows:
-            ptr[name], ld = _rows(t, name, dt, n, w)
-            setattr(d, "ld_" + name, ld)
-    return d, ptr
+        mask = _dp(key_mask, "key_mask", None, n_k)
+    return _AttnDesc(dt, batch, heads_q, heads_kv, head_dim, scale, n_q, n_k, qo, ko, mask), heads_q * head_dim, heads_kv * head_dim
 
 
 def hch_attn_fwd(dtype, Q, K, V, O, lse, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale, workspace,
                  stream=None):
     """Attention inside each shape: Q, O are [n_q][heads_q * head_dim], K, V [n_k][heads_kv * head_dim], or columns of
     wider rows; offsets [batch + 1] int32 on the device; lse [n_q][heads_q] float or None; key_mask [n_k] bytes or None."""
-    d, p = _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale,
-                      (("q", Q), ("o", O)), (("k", K), ("v", V)))
-    _check(load_library().hch_attn_fwd(C.byref(d), p["q"], p["k"], p["v"], p["o"], _dp(lse, "lse", _F32, d.n_q * heads_q),
+    d, wq, wk = _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale)
+    q, d.ld_q = _rows(Q, "Q", dtype, d.n_q, wq)
+    k, d.ld_k = _rows(K, "K", dtype, d.n_k, wk)
+    v, d.ld_v = _rows(V, "V", dtype, d.n_k, wk)
+    o, d.ld_o = _rows(O, "O", dtype, d.n_q, wq)
+    _check(load_library().hch_attn_fwd(C.byref(d), q, k, v, o, _dp(lse, "lse", _F32, d.n_q * heads_q),
                                        _dp(workspace, "workspace"), _nbytes(workspace), _stream(stream)))
 
 
 def hch_attn_bwd(dtype, Q, K, V, O, lse, dO, dQ, dK, dV, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale,
                  workspace, stream=None):
     """Gradients of hch_attn_fwd, from its inputs, its O and its lse."""
-    d, p = _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale,
-                      (("q", Q), ("o", O), ("do", dO), ("dq", dQ)), (("k", K), ("v", V), ("dk", dK), ("dv", dV)))
-    _check(load_library().hch_attn_bwd(C.byref(d), p["q"], p["k"], p["v"], p["o"], _dp(lse, "lse", _F32, d.n_q * heads_q),
-                                       p["do"], p["dq"], p["dk"], p["dv"], _dp(workspace, "workspace"),
-                                       _nbytes(workspace), _stream(stream)))
+    d, wq, wk = _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, head_dim, scale)
+    n_q, n_k = d.n_q, d.n_k
+    q, d.ld_q = _rows(Q, "Q", dtype, n_q, wq)
+    k, d.ld_k = _rows(K, "K", dtype, n_k, wk)
+    v, d.ld_v = _rows(V, "V", dtype, n_k, wk)
+    o, d.ld_o = _rows(O, "O", dtype, n_q, wq)
+    do, d.ld_do = _rows(dO, "dO", dtype, n_q, wq)
+    dq, d.ld_dq = _rows(dQ, "dQ", dtype, n_q, wq)
+    dk, d.ld_dk = _rows(dK, "dK", dtype, n_k, wk)
+    dv, d.ld_dv = _rows(dV, "dV", dtype, n_k, wk)
+    _check(load_library().hch_attn_bwd(C.byref(d), q, k, v, o, _dp(lse, "lse", _F32, n_q * heads_q), do, dq, dk, dv,
+                                       _dp(workspace, "workspace"), _nbytes(workspace), _stream(stream)))
 
 
 def hch_probe_mfma(dtype, iters, workgroups, sink, stream=None):

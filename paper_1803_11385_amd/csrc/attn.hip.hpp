@@ -53,45 +53,64 @@ struct Args {
 };
 
 // ---------------------------------------------------------------------------------------------
-// types
+// how operands are multiplied
 // ---------------------------------------------------------------------------------------------
-template <typename T> struct Mma;
-template <> struct Mma<__bf16> {
-    static constexpr int E = 8;            // elements of 16 bytes
-    // acc += A B over the channels of one 16-byte piece of both halves
-    static __device__ __forceinline__ f32x16 rows(u32x4 a, u32x4 b, f32x16 acc)
-    {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
-    }
-    struct Col { bf16x8 v; };              // 16 streamed rows of the right operand
+// An engine E: T is the type in memory, CHUNK the channels one step of a product over the channels takes, Part one
+// lane's share of that step, PLANES the copies of a tile in LDS, which has rows of STRIDE<D> bytes.
+//   rows   acc += A B over the channels of a chunk; A from the tile, B the lane's own
+//   col    16 streamed rows of the right operand, registers 8 s .. 8 s + 7 of a tile
+//   cols   acc += (16 streamed rows of the tile, transposed) col, channels 32 dt ..
+template <int D> constexpr int stride16 = 2 * D + 16;
+
+// a transposed piece of 16 rows x 32 channels, 16-bit elements; p: the tile's rows 16 s, channels 32 dt, with this
+// lane's offset left16
+__device__ __forceinline__ int left16(int lane, int stride)
+{
+    return (4 * (lane >> 5) + ((lane & 15) >> 2)) * stride + (16 * ((lane >> 4) & 1) + (lane & 3) * 4) * 2;
+}
+__device__ __forceinline__ bf16x8 transposed(const char *p, int stride)
+{
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)(p + 8 * stride));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+__device__ __forceinline__ f32x16 mfma16(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+struct Bf16 {
+    typedef __bf16 T;
+    static constexpr int CHUNK = 16, PLANES = 1;
+    template <int D> static constexpr int STRIDE = stride16<D>;
+    typedef bf16x8 Part;
+    static __device__ __forceinline__ Part part(const __bf16 (&x)[8]) { return __builtin_bit_cast(bf16x8, x); }
+    static __device__ __forceinline__ f32x16 rows(const char *p, int, const Part &b, f32x16 acc) { return mfma16(*(const bf16x8 *)p, b, acc); }
+    typedef bf16x8 Col;
     static __device__ __forceinline__ Col col(const f32x16 &p, int s)
     {
         Col c;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) c.v[j] = (__bf16)p[8 * s + j];
+        for (int j = 0; j < 8; ++j) c[j] = (__bf16)p[8 * s + j];
         return c;
     }
-    // byte offset of this lane's piece of the left operand in a tile with rows of `stride` bytes
-    static __device__ __forceinline__ int left_offset(int lane, int stride)
+    static __device__ __forceinline__ int left(int lane, int stride) { return left16(lane, stride); }
+    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int, int s, int dt, const Col &b, f32x16 acc)
     {
-        return (4 * (lane >> 5) + ((lane & 15) >> 2)) * stride + (16 * ((lane >> 4) & 1) + (lane & 3) * 4) * 2;
+        return mfma16(transposed(tile + 16 * s * stride + 64 * dt, stride), b, acc);
     }
-    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int s, int dt, Col b, f32x16 acc)
-    {
-        const char *p = tile + 16 * s * stride + 64 * dt;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)p);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)(p + 8 * stride));
-        const auto a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b.v, acc, 0, 0, 0);
-    }
+    static __device__ __forceinline__ void store(char *row, int, int piece, u32x4 v) { *(u32x4 *)(row + 16 * piece) = v; }
 };
-template <> struct Mma<float> {
-    static constexpr int E = 4;
-    static __device__ __forceinline__ f32x16 rows(u32x4 a, u32x4 b, f32x16 acc)
+
+// fp32 on the fp32 instruction.
+struct Fp32 {
+    typedef float T;
+    static constexpr int CHUNK = 8, PLANES = 1;
+    template <int D> static constexpr int STRIDE = 4 * D + 16;
+    typedef f32x4 Part;
+    static __device__ __forceinline__ Part part(const float (&x)[4]) { return __builtin_bit_cast(f32x4, x); }
+    static __device__ __forceinline__ f32x16 rows(const char *p, int, const Part &b, f32x16 acc)
     {
-        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+        const f32x4 a = *(const f32x4 *)p;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], y[j], acc, 0, 0, 0);
+        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], acc, 0, 0, 0);
         return acc;
     }
     struct Col { float v[8]; };
@@ -102,14 +121,89 @@ template <> struct Mma<float> {
         for (int j = 0; j < 8; ++j) c.v[j] = p[8 * s + j];
         return c;
     }
-    static __device__ __forceinline__ int left_offset(int lane, int stride) { return 4 * (lane >> 5) * stride + 4 * (lane & 31); }
-    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int s, int dt, Col b, f32x16 acc)
+    static __device__ __forceinline__ int left(int lane, int stride) { return 4 * (lane >> 5) * stride + 4 * (lane & 31); }
+    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int, int s, int dt, const Col &b, f32x16 acc)
     {
         const char *p = tile + 16 * s * stride + 128 * dt;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             acc = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float *)(p + (8 * (j / 4) + j % 4) * stride), b.v[j], acc, 0, 0, 0);
         return acc;
+    }
+    static __device__ __forceinline__ void store(char *row, int, int piece, u32x4 v) { *(u32x4 *)(row + 16 * piece) = v; }
+};
+
+// fp32 on the bf16 instruction: every number is the sum of three bf16 numbers (8 bits each, so exact), and of the nine
+// products of two such sums the six leading ones are taken; what is left out is at most 2^-23 of the
+// product.  Six bf16 steps take 6/16 of the time of the fp32 instruction for the same terms.  (Parts of numbers below 2^-110
+// are lost one by one as they fall below 2^-133; an infinite operand makes its sums NaN.)
+struct Split {
+    typedef float T;
+    static constexpr int CHUNK = 16, PLANES = 3;
+    template <int D> static constexpr int STRIDE = stride16<D>;
+    struct Part { bf16x8 v[3]; };
+    typedef Part Col;
+    static __device__ __forceinline__ uint32_t round2(float a, float b)
+    {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+    }
+    // two numbers as three packed pairs; both differences are exact
+    static __device__ __forceinline__ void cut(float a, float b, uint32_t (&v)[3])
+    {
+        v[0] = round2(a, b);
+        const float ra = a - __uint_as_float(v[0] << 16), rb = b - __uint_as_float(v[0] & 0xffff0000u);
+        v[1] = round2(ra, rb);
+        v[2] = round2(ra - __uint_as_float(v[1] << 16), rb - __uint_as_float(v[1] & 0xffff0000u));
+    }
+    static __device__ __forceinline__ Part part(const float (&x)[8])
+    {
+        u32x4 t[3];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t v[3];
+            cut(x[2 * j], x[2 * j + 1], v);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) t[k][j] = v[k];
+        }
+        Part p;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) p.v[k] = __builtin_bit_cast(bf16x8, t[k]);
+        return p;
+    }
+    static __device__ __forceinline__ f32x16 six(const bf16x8 (&a)[3], const bf16x8 (&b)[3], f32x16 acc)
+    {
+        constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};      // the smallest first
+#pragma unroll
+        for (int i = 0; i < 6; ++i) acc = mfma16(a[PA[i]], b[PB[i]], acc);
+        return acc;
+    }
+    static __device__ __forceinline__ f32x16 rows(const char *p, int plane, const Part &b, f32x16 acc)
+    {
+        const bf16x8 a[3] = {*(const bf16x8 *)p, *(const bf16x8 *)(p + plane), *(const bf16x8 *)(p + 2 * plane)};
+        return six(a, b.v, acc);
+    }
+    static __device__ __forceinline__ Col col(const f32x16 &p, int s)
+    {
+        const float x[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
+        return part(x);
+    }
+    static __device__ __forceinline__ int left(int lane, int stride) { return left16(lane, stride); }
+    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int plane, int s, int dt, const Col &b, f32x16 acc)
+    {
+        const char *p = tile + 16 * s * stride + 64 * dt;
+        const bf16x8 a[3] = {transposed(p, stride), transposed(p + plane, stride), transposed(p + 2 * plane, stride)};
+        return six(a, b.v, acc);
+    }
+    static __device__ __forceinline__ void store(char *row, int plane, int piece, u32x4 v)
+    {
+        const f32x4 x = __builtin_bit_cast(f32x4, v);
+        uint32_t lo[3], hi[3];
+        cut(x[0], x[1], lo);
+        cut(x[2], x[3], hi);
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *(u32x2 *)(row + k * plane + 8 * piece) = u32x2{lo[k], hi[k]};
     }
 };
 
@@ -165,8 +259,8 @@ inline int64_t slots_of(int64_t n, int rows_each, int size, int batch) { return 
 // ---------------------------------------------------------------------------------------------
 // tiles
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D> struct Tile {
-    static constexpr int STRIDE = D * (int)sizeof(T) + 16, CHUNKS = D * (int)sizeof(T) / 32, DT = D / 32;
+template <typename E, int D> struct Tile {
+    static constexpr int STRIDE = E::template STRIDE<D>, CHUNKS = D / E::CHUNK, DT = D / 32;
 };
 
 // 16 bytes from element 0 .. of a row, `have` of them there; zeros behind
@@ -188,7 +282,8 @@ template <typename T> __device__ __forceinline__ u32x4 load_elements(__amdgpu_bu
 }
 
 // The part of a tile of ROWS rows that a thread moves from memory to LDS: fixed pieces of 16 bytes.
-template <typename T, int D, int ROWS, int THREADS> struct Stage {
+template <typename E, int D, int ROWS, int THREADS> struct Stage {
+    typedef typename E::T T;
     static constexpr int PER_ROW = D * (int)sizeof(T) / 16, PIECES = ROWS * PER_ROW, N = (PIECES + THREADS - 1) / THREADS;
     u32x4 r[N];
     // rows [row0, row0 + ROWS) of a matrix that ends before row `end`; `base`: channel 0 of row 0.  Rows and channels that
@@ -200,7 +295,7 @@ template <typename T, int D, int ROWS, int THREADS> struct Stage {
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(base + row0 * ld), 0, bytes, SRD3);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int p = tid + i * THREADS, row = p / PER_ROW, e = (p - row * PER_ROW) * Mma<T>::E;
+            const int p = tid + i * THREADS, row = p / PER_ROW, e = (p - row * PER_ROW) * (16 / (int)sizeof(T));
             const int have = PIECES % THREADS && p >= PIECES ? 0 : d - e;
             const int offset = (int)(row * ld + e) * (int)sizeof(T);
             if (vec) r[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, have > 0 ? offset : OUT, 0, 0));
@@ -216,51 +311,53 @@ template <typename T, int D, int ROWS, int THREADS> struct Stage {
             if (PIECES % THREADS && p >= PIECES) continue;
             u32x4 v = r[i];
             if (keep && !(keep[row >> 6] >> (row & 63) & 1)) v = u32x4{0, 0, 0, 0};
-            *(u32x4 *)(tile + row * Tile<T, D>::STRIDE + col * 16) = v;
+            E::store(tile + row * Tile<E, D>::STRIDE, ROWS * Tile<E, D>::STRIDE, col, v);
         }
     }
 };
 
-// A wavefront's own 32 rows as an operand of products over the channels: the pieces at bytes 32 s + 16 h of a row.
-template <typename T, int D> struct Own {
-    u32x4 v[Tile<T, D>::CHUNKS];
-    __device__ __forceinline__ void load(const T *row, bool valid, int d, bool vec, int h)
+// `count` elements of a row from element e on; zeros where there are none
+template <typename T, int N> __device__ __forceinline__ void load_piece(const T *row, int e, bool valid, int d, bool vec, T (&x)[N])
+{
+    if (valid && vec && e < d) {
+#pragma unroll
+        for (int i = 0; i < N * (int)sizeof(T) / 16; ++i) __builtin_memcpy((char *)x + 16 * i, (const char *)(row + e) + 16 * i, 16);
+    } else
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = valid && e + j < d ? row[e + j] : (T)0.f;
+}
+
+// A wavefront's own 32 rows as an operand of products over the channels: of each chunk the half's share.
+template <typename E, int D> struct Own {
+    typename E::Part v[Tile<E, D>::CHUNKS];
+    __device__ __forceinline__ void load(const typename E::T *row, bool valid, int d, bool vec, int h)
     {
 #pragma unroll
-        for (int s = 0; s < Tile<T, D>::CHUNKS; ++s) {
-            const int e = (32 * s + 16 * h) / (int)sizeof(T);
-            u32x4 x = {0, 0, 0, 0};
-            if (valid && e < d) {
-                if (vec) x = *(const u32x4 *)(row + e);
-                else {
-                    T t[Mma<T>::E];
-#pragma unroll
-                    for (int j = 0; j < Mma<T>::E; ++j) t[j] = e + j < d ? row[e + j] : (T)0.f;
-                    __builtin_memcpy(&x, t, 16);
-                }
-            }
-            v[s] = x;
+        for (int s = 0; s < Tile<E, D>::CHUNKS; ++s) {
+            typename E::T x[E::CHUNK / 2];
+            load_piece(row, E::CHUNK * s + E::CHUNK / 2 * h, valid, d, vec && d % (E::CHUNK / 2) == 0, x);
+            v[s] = E::part(x);
         }
     }
 };
 
-// scores of 32 streamed rows against the own rows
-template <typename T, int D> __device__ __forceinline__ f32x16 product(const char *tile, const Own<T, D> &own, int lane, f32x16 acc)
+// scores of 32 streamed rows against the own rows; plane: bytes between the planes of the tile
+template <typename E, int D> __device__ __forceinline__ f32x16 product(const char *tile, int plane, const Own<E, D> &own, int lane, f32x16 acc)
 {
-    const char *p = tile + (lane & 31) * Tile<T, D>::STRIDE + 16 * (lane >> 5);
+    const char *p = tile + (lane & 31) * Tile<E, D>::STRIDE + 16 * (lane >> 5);       // a chunk is 32 bytes of a plane
 #pragma unroll
-    for (int s = 0; s < Tile<T, D>::CHUNKS; ++s) acc = Mma<T>::rows(*(const u32x4 *)(p + 32 * s), own.v[s], acc);
+    for (int s = 0; s < Tile<E, D>::CHUNKS; ++s) acc = E::rows(p + 32 * s, plane, own.v[s], acc);
     return acc;
 }
 // acc[dt] += (32 streamed rows, transposed) p
-template <typename T, int D>
-__device__ __forceinline__ void fold(const char *tile, const f32x16 &p, int left, f32x16 (&acc)[Tile<T, D>::DT])
+template <typename E, int D>
+__device__ __forceinline__ void fold(const char *tile, int plane, const f32x16 &p, int left, f32x16 (&acc)[Tile<E, D>::DT])
 {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const typename Mma<T>::Col b = Mma<T>::col(p, s);
+        const typename E::Col b = E::col(p, s);
 #pragma unroll
-        for (int dt = 0; dt < Tile<T, D>::DT; ++dt) acc[dt] = Mma<T>::cols(tile + left, Tile<T, D>::STRIDE, s, dt, b, acc[dt]);
+        for (int dt = 0; dt < Tile<E, D>::DT; ++dt) acc[dt] = E::cols(tile + left, Tile<E, D>::STRIDE, plane, s, dt, b, acc[dt]);
     }
 }
 // this lane's row of a result: channel 32 dt + 8 (r / 4) + 4 h + r % 4
@@ -289,10 +386,11 @@ __device__ __forceinline__ int key_byte(const uint8_t *mask, int key, int end) {
 
 // Sizes of the passes over the keys.  QW wavefronts have rows of their own and KW = WAVES / QW share a row tile's keys:
 // 4 x 1 for long queries, 1 x 4 where a shape has few query rows and the keys are what there is to read.
-template <typename T, int D, int QW> struct Keys {
-    static constexpr int WAVES = QW == 1 && D * sizeof(T) > 256 ? 2 : 4, THREADS = 64 * WAVES, KW = WAVES / QW, BQ = 32 * QW;
-    static constexpr int BK = QW == 1 ? 32 * KW : sizeof(T) == 2 ? 64 : 32, NT = BK / 32 / KW;
-    static constexpr int BUFFERS = QW == 1 ? 1 : 2, TILE = BK * Tile<T, D>::STRIDE;
+template <typename E, int D, int QW> struct Keys {
+    static constexpr int WAVES = QW == 1 && D * sizeof(typename E::T) > 256 ? 2 : 4, THREADS = 64 * WAVES, KW = WAVES / QW, BQ = 32 * QW;
+    static constexpr int BK = QW == 1 ? 32 * KW : E::PLANES == 1 && sizeof(typename E::T) == 2 ? 64 : 32, NT = BK / 32 / KW;
+    static constexpr int PLANE = BK * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE;
+    static constexpr int BUFFERS = QW == 1 || 4 * TILE > 80 * 1024 ? 1 : 2;     // two where two workgroups still share a compute unit
     static constexpr int WORDS = (BK + 63) / 64;
     static constexpr int LDS = 2 * BUFFERS * TILE;
 };
@@ -302,11 +400,12 @@ template <typename T, int D, int QW> struct Keys {
 // ---------------------------------------------------------------------------------------------
 // Query rows of the heads that share a key head are one list, row = token * group + (head within the group), so that
 // a tile of keys serves the whole group.
-template <typename T, int D, int QW>
-__global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_fwd_kernel(Args a)
+template <typename E, int D, int QW>
+__global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Args a)
 {
-    typedef Keys<T, D, QW> S;
-    typedef Tile<T, D> L;
+    typedef Keys<E, D, QW> S;
+    typedef Tile<E, D> L;
+    typedef typename E::T T;
     __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave : 0;
@@ -323,7 +422,7 @@ __global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_fwd_kernel(Arg
     const bool valid = row < rows;
     const int64_t token = valid ? q.begin + row / a.group : q.begin;
     const int head = kvh * a.group + (valid ? (int)(row % a.group) : 0);
-    Own<T, D> own;
+    Own<E, D> own;
     own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, valid, a.d, a.vec, h);
 
     const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
@@ -331,14 +430,14 @@ __global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_fwd_kernel(Arg
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
     const uint8_t *mask = a.mask ? a.mask + k.begin : nullptr;
     const int len = k.end - k.begin;
-    const int left = Mma<T>::left_offset(lane, L::STRIDE);
+    const int left = E::left(lane, L::STRIDE);
 
     f32x16 acc[L::DT];
 #pragma unroll
     for (int dt = 0; dt < L::DT; ++dt) acc[dt] = f32x16{};
     float m = -INFINITY, l = 0.f;
 
-    Stage<T, D, S::BK, S::THREADS> ks, vs;
+    Stage<E, D, S::BK, S::THREADS> ks, vs;
     int seen[S::WORDS];
     auto load = [&](int t) {
         ks.load(kp, a.ld_k, t * S::BK, len, a.d, a.vec, tid);
@@ -368,7 +467,7 @@ __global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_fwd_kernel(Arg
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) {
             const int sub = QW == 1 ? kw : i;
-            s[i] = product<T, D>(kt + 32 * sub * L::STRIDE, own, lane, f32x16{});
+            s[i] = product<E, D>(kt + 32 * sub * L::STRIDE, S::PLANE, own, lane, f32x16{});
             if (!all) {
                 const uint32_t bits = (uint32_t)(keep[sub >> 1] >> (32 * (sub & 1))) >> (4 * h);
 #pragma unroll
@@ -398,7 +497,7 @@ __global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_fwd_kernel(Arg
                 s[i][r] = exp2_fast(__builtin_fmaf(s[i][r], a.c, -base));
                 l += s[i][r];
             }
-            fold<T, D>(vt + 32 * (QW == 1 ? kw : i) * L::STRIDE, s[i], left, acc);
+            fold<E, D>(vt + 32 * (QW == 1 ? kw : i) * L::STRIDE, S::PLANE, s[i], left, acc);
         }
     }
     l += other_half(l);
@@ -449,67 +548,86 @@ __global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_fwd_kernel(Arg
     }
 }
 
-// Joins the splits of a row: thread groups of 16 lanes over the channels, the splits dealt to the 16 groups of a workgroup.
-template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(Args a)
+// Joins the splits of a row: G groups of 32 lanes deal the splits among them, a lane has 4 channels.  8 groups for a row
+// where there are few rows of many splits; else a group for each (10778 rows x 2 heads of 3 splits: 34 -> 5 us).
+template <typename T, int G> __global__ __launch_bounds__(256) void attn_join_kernel(Args a)
 {
-    __shared__ float sums[16][128];
-    __shared__ float2 ml[16];
-    const int64_t at = blockIdx.x, rows = a.nq * a.hq;
-    const int x = threadIdx.x & 15, g = threadIdx.x >> 4;
-    float m = -INFINITY;
-    for (int s = g; s < a.splits; s += 16) m = fmaxf(m, a.ml[s * rows + at].x);
-    float l = 0.f, acc[8] = {};
-    for (int s = g; s < a.splits; s += 16) {
-        const float2 v = a.ml[s * rows + at];
-        if (!(v.y > 0.f || v.y != v.y)) continue;       // a split without a key has written no sums
-        const float f = exp2_fast(v.x - m);
-        l += f * v.y;
+    __shared__ __align__(16) float sums[8][128];
+    __shared__ float2 ml[8];
+    const int x = threadIdx.x & 31, group = threadIdx.x >> 5, g = group % G;
+    const int64_t rows = a.nq * a.hq, at = (int64_t)blockIdx.x * (8 / G) + group / G;
+    const bool there = at < rows, whole = a.d % 4 == 0;
+    float m = -INFINITY, l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (there) {
+        for (int s = g; s < a.splits; s += G) m = fmaxf(m, a.ml[s * rows + at].x);
+        for (int s = g; s < a.splits; s += G) {
+            const float2 v = a.ml[s * rows + at];
+            if (!(v.y > 0.f || v.y != v.y)) continue;   // a split without a key has written no sums
+            const float f = exp2_fast(v.x - m);
+            l += f * v.y;
+            const float *p = a.part + (s * rows + at) * a.d + 4 * x;
+            if (4 * x < a.d) {
+                if (whole) acc += f * *(const f32x4 *)p;
+                else
 #pragma unroll
-        for (int j = 0; j < 8; ++j) if (x + 16 * j < a.d) acc[j] += f * a.part[(s * rows + at) * a.d + x + 16 * j];
+                    for (int j = 0; j < 4; ++j) if (4 * x + j < a.d) acc[j] += f * p[j];
+            }
+        }
     }
+    if constexpr (G > 1) {
+        *(f32x4 *)&sums[g][4 * x] = acc;
+        if (x == 0) ml[g] = make_float2(m, l);
+        __syncthreads();
+        if (g) return;
+        m = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[g][x + 16 * j] = acc[j];
-    if (x == 0) ml[g] = make_float2(m, l);
-    __syncthreads();
-    m = -INFINITY;
-    for (int i = 0; i < 16; ++i) m = fmaxf(m, ml[i].x);
-    l = 0.f;
-    for (int i = 0; i < 16; ++i) l += ml[i].y != 0.f ? ml[i].y * exp2_fast(ml[i].x - m) : 0.f;
+        for (int i = 0; i < G; ++i) m = fmaxf(m, ml[i].x);
+        l = 0.f;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            if (ml[i].y == 0.f) continue;
+            const float f = exp2_fast(ml[i].x - m);
+            l += f * ml[i].y;
+            acc += f * *(const f32x4 *)&sums[i][4 * x];
+        }
+    }
+    if (!there) return;
     const int64_t token = at / a.hq;
-    const int head = (int)(at - token * a.hq);
     const bool some = l > 0.f || l != l;
-    if (threadIdx.x < a.d) {
-        float t = 0.f;
-        for (int i = 0; i < 16; ++i) if (ml[i].y != 0.f) t += sums[i][threadIdx.x] * exp2_fast(ml[i].x - m);
-        ((T *)a.Ow)[token * a.ld_o + (int64_t)head * a.d + threadIdx.x] = (T)(some ? t / l : 0.f);
-    }
-    if (a.lse && threadIdx.x == 0) a.lse[at] = some ? m * LN2 + logf(l) : -INFINITY;
+    T *o = (T *)a.Ow + token * a.ld_o + (at - token * a.hq) * a.d;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) if (4 * x + j < a.d) o[4 * x + j] = (T)(some ? acc[j] / l : 0.f);
+    if (a.lse && x == 0) a.lse[at] = some ? m * LN2 + logf(l) : -INFINITY;
 }
 
 // ---------------------------------------------------------------------------------------------
 // backward
 // ---------------------------------------------------------------------------------------------
-// a . b of this lane's row: 16-byte pieces held by the two halves
-template <typename T, int D> __device__ __forceinline__ float row_dot(const Own<T, D> &a, const Own<T, D> &b)
+// a . b of this lane's row; each half takes every other piece
+template <typename T, int D> __device__ __forceinline__ float row_dot(const T *a, const T *b, bool valid, int d, bool vec, int h)
 {
+    constexpr int N = 16 / (int)sizeof(T);
     float t = 0.f;
 #pragma unroll
-    for (int s = 0; s < Tile<T, D>::CHUNKS; ++s) {
-        T x[Mma<T>::E], y[Mma<T>::E];
-        __builtin_memcpy(x, &a.v[s], 16);
-        __builtin_memcpy(y, &b.v[s], 16);
+    for (int s = 0; s < D / N / 2; ++s) {
+        T x[N], y[N];
+        load_piece(a, (2 * s + h) * N, valid, d, vec, x);
+        load_piece(b, (2 * s + h) * N, valid, d, vec, y);
 #pragma unroll
-        for (int j = 0; j < Mma<T>::E; ++j) t += (float)x[j] * (float)y[j];
+        for (int j = 0; j < N; ++j) t += (float)x[j] * (float)y[j];
     }
     return t + other_half(t);
 }
 
 // dQ, and D for the pass over the keys: the walk of the forward kernel.
-template <typename T, int D, int QW>
-__global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_bwd_dq_kernel(Args a)
+template <typename E, int D, int QW>
+__global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(Args a)
 {
-    typedef Keys<T, D, QW> S;
-    typedef Tile<T, D> L;
+    typedef Keys<E, D, QW> S;
+    typedef Tile<E, D> L;
+    typedef typename E::T T;
     __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave : 0;
@@ -530,15 +648,11 @@ __global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_bwd_dq_kernel(
     const float lse = a.lse[at];
     const bool part = valid && lse != -INFINITY;        // a row that saw no key: its gradient is zero, whatever dO holds
     const float lse2 = part ? lse * LOG2E : INFINITY;
-    Own<T, D> own, grad;
+    Own<E, D> own, grad;
     own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, part, a.d, a.vec, h);
     grad.load((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d, part, a.d, a.vec, h);
-    float delta;
-    {
-        Own<T, D> out;
-        out.load((const T *)a.O + token * a.ld_o + (int64_t)head * a.d, part, a.d, a.vec, h);
-        delta = row_dot<T, D>(grad, out);
-    }
+    const float delta = row_dot<T, D>((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d,
+                                      (const T *)a.O + token * a.ld_o + (int64_t)head * a.d, part, a.d, a.vec, h);
     if (valid && split == 0 && kw == 0 && h == 0) a.delta[at] = delta;
 
     const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
@@ -546,12 +660,12 @@ __global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_bwd_dq_kernel(
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
     const uint8_t *mask = a.mask ? a.mask + k.begin : nullptr;
     const int len = k.end - k.begin;
-    const int left = Mma<T>::left_offset(lane, L::STRIDE);
+    const int left = E::left(lane, L::STRIDE);
 
     f32x16 acc[L::DT];
 #pragma unroll
     for (int dt = 0; dt < L::DT; ++dt) acc[dt] = f32x16{};
-    Stage<T, D, S::BK, S::THREADS> ks, vs;
+    Stage<E, D, S::BK, S::THREADS> ks, vs;
     int seen[S::WORDS];
     auto load = [&](int t) {
         ks.load(kp, a.ld_k, t * S::BK, len, a.d, a.vec, tid);
@@ -577,11 +691,11 @@ __global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_bwd_dq_kernel(
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) {
             const int sub = QW == 1 ? kw : i;
-            f32x16 s = product<T, D>(kt + 32 * sub * L::STRIDE, own, lane, f32x16{});
+            f32x16 s = product<E, D>(kt + 32 * sub * L::STRIDE, S::PLANE, own, lane, f32x16{});
             f32x16 g;
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[r] = -delta;
-            g = product<T, D>(vt + 32 * sub * L::STRIDE, grad, lane, g);
+            g = product<E, D>(vt + 32 * sub * L::STRIDE, S::PLANE, grad, lane, g);
             if (!all) {
                 const uint32_t bits = (uint32_t)(keep[sub >> 1] >> (32 * (sub & 1))) >> (4 * h);
 #pragma unroll
@@ -589,7 +703,7 @@ __global__ __launch_bounds__((Keys<T, D, QW>::THREADS)) void attn_bwd_dq_kernel(
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[r] *= exp2_fast(__builtin_fmaf(s[r], a.c, -lse2));
-            fold<T, D>(kt + 32 * sub * L::STRIDE, g, left, acc);
+            fold<E, D>(kt + 32 * sub * L::STRIDE, S::PLANE, g, left, acc);
         }
     }
     if constexpr (QW == 1) {
@@ -633,15 +747,17 @@ template <typename T> __global__ __launch_bounds__(256) void attn_bwd_join_kerne
 
 // dK and dV: a wavefront has 32 keys, the queries of all heads that share their head stream past, one head after
 // the other, so the sum over them is taken in registers in a fixed order.
-template <typename T, int D> struct Queries {
-    static constexpr int THREADS = 256, BK = 128, BR = sizeof(T) == 2 ? 64 : 32, NT = BR / 32, TILE = BR * Tile<T, D>::STRIDE;
-    static constexpr int BUFFER = 2 * TILE + 2 * BR * 4, LDS = 2 * BUFFER;
+template <typename E, int D> struct Queries {
+    static constexpr int THREADS = 256, BK = 128, BR = E::PLANES == 1 && sizeof(typename E::T) == 2 ? 64 : 32, NT = BR / 32;
+    static constexpr int PLANE = BR * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE, BUFFER = 2 * TILE + 2 * BR * 4;
+    static constexpr int BUFFERS = 2 * BUFFER > 80 * 1024 ? 1 : 2, LDS = BUFFERS * BUFFER;
 };
-template <typename T, int D>
+template <typename E, int D>
 __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(Args a)
 {
-    typedef Queries<T, D> S;
-    typedef Tile<T, D> L;
+    typedef Queries<E, D> S;
+    typedef Tile<E, D> L;
+    typedef typename E::T T;
     __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int w = work_item(blockIdx.x);
@@ -654,17 +770,17 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(Args a)
 
     const int64_t key = k.begin + (int64_t)tile * S::BK + 32 * wave + (lane & 31);
     const bool valid = key < k.end, seen = valid && (!a.mask || a.mask[key]);
-    Own<T, D> kk, vv;
+    Own<E, D> kk, vv;
     kk.load((const T *)a.K + (valid ? key : 0) * a.ld_k + (int64_t)kvh * a.d, seen, a.d, a.vec, h);
     vv.load((const T *)a.V + (valid ? key : 0) * a.ld_v + (int64_t)kvh * a.d, seen, a.d, a.vec, h);
 
     const int len = q.end - q.begin, tiles = (len + S::BR - 1) / S::BR, steps = tiles * a.group;
-    const int left = Mma<T>::left_offset(lane, L::STRIDE);
+    const int left = E::left(lane, L::STRIDE);
     f32x16 dk[L::DT], dv[L::DT];
 #pragma unroll
     for (int dt = 0; dt < L::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
 
-    Stage<T, D, S::BR, S::THREADS> qs, gs;
+    Stage<E, D, S::BR, S::THREADS> qs, gs;
     float lse = 0.f, delta = 0.f;
     auto load = [&](int head, int t) {
         qs.load((const T *)a.Q + q.begin * a.ld_q + (int64_t)head * a.d, a.ld_q, t * S::BR, len, a.d, a.vec, tid);
@@ -679,8 +795,9 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(Args a)
     int head = kvh * a.group, t = 0;
     if (steps) load(head, 0);
     for (int step = 0; step < steps; ++step) {
-        char *qt = lds + (step & 1) * S::BUFFER, *gt = qt + S::TILE;
+        char *qt = lds + (S::BUFFERS == 2 ? (step & 1) * S::BUFFER : 0), *gt = qt + S::TILE;
         float *stat = (float *)(gt + S::TILE);
+        if (S::BUFFERS == 1) __syncthreads();
         qs.store(qt, tid, nullptr);
         gs.store(gt, tid, nullptr);
         if (tid < S::BR) {
@@ -692,7 +809,7 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(Args a)
         if (step + 1 < steps) load(head, t);
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) {
-            f32x16 p = product<T, D>(qt + 32 * i * L::STRIDE, kk, lane, f32x16{});
+            f32x16 p = product<E, D>(qt + 32 * i * L::STRIDE, S::PLANE, kk, lane, f32x16{});
             f32x16 g;
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
@@ -704,11 +821,11 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(Args a)
                     g[r + j] = y[j];
                 }
             }
-            g = product<T, D>(gt + 32 * i * L::STRIDE, vv, lane, g);
-            fold<T, D>(gt + 32 * i * L::STRIDE, p, left, dv);
+            g = product<E, D>(gt + 32 * i * L::STRIDE, S::PLANE, vv, lane, g);
+            fold<E, D>(gt + 32 * i * L::STRIDE, S::PLANE, p, left, dv);
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[r] *= p[r];
-            fold<T, D>(qt + 32 * i * L::STRIDE, g, left, dk);
+            fold<E, D>(qt + 32 * i * L::STRIDE, S::PLANE, g, left, dk);
         }
     }
     if (!valid) return;

@@ -13,6 +13,10 @@ template <typename T> hch_status launch_bwd_dq(const Args &a, bool few, double b
 template <typename T> hch_status launch_bwd_dkv(const Args &a, double bytes, double flops, hipStream_t s);
 
 #ifdef HCH_ATTN_TYPE
+// The engines of a type: for passes that the products bound, and for the form for few queries, which memory bounds.
+template <typename T> struct Engine { typedef Bf16 Many, Few; };
+template <> struct Engine<float> { typedef Split Many; typedef Fp32 Few; };
+
 template <typename F> void with_width(int d, F &&f)
 {
     if (d <= 32) f(std::integral_constant<int, 32>{});
@@ -28,11 +32,11 @@ template <typename T> hch_status launch_fwd(const Args &a, bool few, double byte
         with_width(a.d, [&](auto w) {
             constexpr int D = decltype(w)::value;
             if (few) {
-                constexpr auto kernel = attn_fwd_kernel<T, D, 1>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(Keys<T, D, 1>::THREADS), 0, s, a);
+                constexpr auto kernel = attn_fwd_kernel<typename Engine<T>::Few, D, 1>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<typename Engine<T>::Few, D, 1>::THREADS)), 0, s, a);
             } else {
-                constexpr auto kernel = attn_fwd_kernel<T, D, 4>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(Keys<T, D, 4>::THREADS), 0, s, a);
+                constexpr auto kernel = attn_fwd_kernel<typename Engine<T>::Many, D, 4>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<typename Engine<T>::Many, D, 4>::THREADS)), 0, s, a);
             }
         });
     }
@@ -40,8 +44,11 @@ template <typename T> hch_status launch_fwd(const Args &a, bool few, double byte
     if (a.splits > 1) {
         {
             LaunchTimer lt(HCH_KERNEL_ID("attn_join_kernel"), s, (double)a.splits * a.nq * a.hq * (4 * a.d + 8), 0.0);
-            constexpr auto kernel = attn_join_kernel<T>;
-            HCH_LAUNCH(kernel, dim3((unsigned)(a.nq * a.hq)), dim3(256), 0, s, a);
+            const int64_t rows = a.nq * a.hq;
+            constexpr auto one = attn_join_kernel<T, 1>;
+            constexpr auto eight = attn_join_kernel<T, 8>;
+            if (a.splits <= 8 || rows >= 4096) HCH_LAUNCH(one, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, a);
+            else HCH_LAUNCH(eight, dim3((unsigned)rows), dim3(256), 0, s, a);
         }
         HCH_LAUNCH_CHECK("attn_join_kernel");
     }
@@ -55,11 +62,11 @@ template <typename T> hch_status launch_bwd_dq(const Args &a, bool few, double b
         with_width(a.d, [&](auto w) {
             constexpr int D = decltype(w)::value;
             if (few) {
-                constexpr auto kernel = attn_bwd_dq_kernel<T, D, 1>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(Keys<T, D, 1>::THREADS), 0, s, a);
+                constexpr auto kernel = attn_bwd_dq_kernel<typename Engine<T>::Few, D, 1>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<typename Engine<T>::Few, D, 1>::THREADS)), 0, s, a);
             } else {
-                constexpr auto kernel = attn_bwd_dq_kernel<T, D, 4>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(Keys<T, D, 4>::THREADS), 0, s, a);
+                constexpr auto kernel = attn_bwd_dq_kernel<typename Engine<T>::Many, D, 4>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<typename Engine<T>::Many, D, 4>::THREADS)), 0, s, a);
             }
         });
     }
@@ -80,7 +87,7 @@ template <typename T> hch_status launch_bwd_dkv(const Args &a, double bytes, dou
     {
         LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_dkv_kernel"), s, bytes, flops);
         with_width(a.d, [&](auto w) {
-            constexpr auto kernel = attn_bwd_dkv_kernel<T, decltype(w)::value>;
+            constexpr auto kernel = attn_bwd_dkv_kernel<typename Engine<T>::Many, decltype(w)::value>;
             HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(256), 0, s, a);
         });
     }
