@@ -5,8 +5,7 @@
 //   backward  p_ij = exp(s_ij - lse_i);  D_i = dO_i . o_i;  dS_ij = p_ij (dO_i . v_j - D_i)
 //             dV_j = sum_i p_ij dO_i;  dK_j = scale sum_i dS_ij q_i;  dQ_i = scale sum_j dS_ij k_j
 //
-// All kernels multiply 32 x 32 tiles with the 32x32 instructions (bf16: 16 terms, fp32: 2 terms at a time).  The
-// scores are always formed so that what stays fixed for a wavefront (its queries, or in the pass over keys its keys)
+// All kernels multiply 32 x 32 tiles with the 32x32x16 bf16 instruction.  The scores are always formed so that what stays fixed for a wavefront (its queries, or in the pass over keys its keys)
 // is the column, i.e. the lane, and what streams past is the row, i.e. the register.  Then
 //   * a row's maximum and sum are sums over a lane's own registers and one exchange between the two
 //     half-wavefronts, and what scales a query is one number per lane;
@@ -14,9 +13,8 @@
 //     over the streamed rows: register r of half h is row 8 (r / 4) + 4 h + r % 4, and the left operand is read
 //     in the same order, so nothing is exchanged between the products.
 // The streamed tile lies row by row in LDS, 16 bytes between rows: ds_read_b128 for products over the channels
-// (rows of 16 consecutive bytes), for products over the rows with bf16 the transposing ds_read_b64_tr_b16 (16
-// lanes give the addresses of 4 rows x 16 channels and get 4 rows of one channel each), with fp32 plain
-// reads across the lanes.
+// (16 consecutive bytes of a row), for products over the rows the transposing ds_read_b64_tr_b16 (16 lanes give the
+// addresses of 4 rows x 16 channels and get 4 rows of one channel each).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -55,12 +53,12 @@ struct Args {
 // ---------------------------------------------------------------------------------------------
 // how operands are multiplied
 // ---------------------------------------------------------------------------------------------
-// An engine E: T is the type in memory, CHUNK the channels one step of a product over the channels takes, Part one
-// lane's share of that step, PLANES the copies of a tile in LDS, which has rows of STRIDE<D> bytes.
+// An engine E: T is the type in memory, Part one lane's share of a chunk of 16 channels, PLANES the parts a tile has in
+// LDS.
 //   rows   acc += A B over the channels of a chunk; A from the tile, B the lane's own
 //   col    16 streamed rows of the right operand, registers 8 s .. 8 s + 7 of a tile
 //   cols   acc += (16 streamed rows of the tile, transposed) col, channels 32 dt ..
-template <int D> constexpr int stride16 = 2 * D + 16;
+constexpr int CHUNK = 16;
 
 // a transposed piece of 16 rows x 32 channels, 16-bit elements; p: the tile's rows 16 s, channels 32 dt, with this
 // lane's offset left16
@@ -78,8 +76,7 @@ __device__ __forceinline__ f32x16 mfma16(bf16x8 a, bf16x8 b, f32x16 c) { return 
 
 struct Bf16 {
     typedef __bf16 T;
-    static constexpr int CHUNK = 16, PLANES = 1;
-    template <int D> static constexpr int STRIDE = stride16<D>;
+    static constexpr int PLANES = 1;
     typedef bf16x8 Part;
     static __device__ __forceinline__ Part part(const __bf16 (&x)[8]) { return __builtin_bit_cast(bf16x8, x); }
     static __device__ __forceinline__ f32x16 rows(const char *p, int, const Part &b, f32x16 acc) { return mfma16(*(const bf16x8 *)p, b, acc); }
@@ -91,44 +88,9 @@ struct Bf16 {
         for (int j = 0; j < 8; ++j) c[j] = (__bf16)p[8 * s + j];
         return c;
     }
-    static __device__ __forceinline__ int left(int lane, int stride) { return left16(lane, stride); }
     static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int, int s, int dt, const Col &b, f32x16 acc)
     {
         return mfma16(transposed(tile + 16 * s * stride + 64 * dt, stride), b, acc);
-    }
-    static __device__ __forceinline__ void store(char *row, int, int piece, u32x4 v) { *(u32x4 *)(row + 16 * piece) = v; }
-};
-
-// fp32 on the fp32 instruction.
-struct Fp32 {
-    typedef float T;
-    static constexpr int CHUNK = 8, PLANES = 1;
-    template <int D> static constexpr int STRIDE = 4 * D + 16;
-    typedef f32x4 Part;
-    static __device__ __forceinline__ Part part(const float (&x)[4]) { return __builtin_bit_cast(f32x4, x); }
-    static __device__ __forceinline__ f32x16 rows(const char *p, int, const Part &b, f32x16 acc)
-    {
-        const f32x4 a = *(const f32x4 *)p;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], acc, 0, 0, 0);
-        return acc;
-    }
-    struct Col { float v[8]; };
-    static __device__ __forceinline__ Col col(const f32x16 &p, int s)
-    {
-        Col c;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) c.v[j] = p[8 * s + j];
-        return c;
-    }
-    static __device__ __forceinline__ int left(int lane, int stride) { return 4 * (lane >> 5) * stride + 4 * (lane & 31); }
-    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int, int s, int dt, const Col &b, f32x16 acc)
-    {
-        const char *p = tile + 16 * s * stride + 128 * dt;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float *)(p + (8 * (j / 4) + j % 4) * stride), b.v[j], acc, 0, 0, 0);
-        return acc;
     }
     static __device__ __forceinline__ void store(char *row, int, int piece, u32x4 v) { *(u32x4 *)(row + 16 * piece) = v; }
 };
@@ -139,8 +101,7 @@ struct Fp32 {
 // are lost one by one as they fall below 2^-133; an infinite operand makes its sums NaN.)
 struct Split {
     typedef float T;
-    static constexpr int CHUNK = 16, PLANES = 3;
-    template <int D> static constexpr int STRIDE = stride16<D>;
+    static constexpr int PLANES = 3;
     struct Part { bf16x8 v[3]; };
     typedef Part Col;
     static __device__ __forceinline__ uint32_t round2(float a, float b)
@@ -188,7 +149,6 @@ struct Split {
         const float x[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
         return part(x);
     }
-    static __device__ __forceinline__ int left(int lane, int stride) { return left16(lane, stride); }
     static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int plane, int s, int dt, const Col &b, f32x16 acc)
     {
         const char *p = tile + 16 * s * stride + 64 * dt;
@@ -260,7 +220,7 @@ inline int64_t slots_of(int64_t n, int rows_each, int size, int batch) { return 
 // tiles
 // ---------------------------------------------------------------------------------------------
 template <typename E, int D> struct Tile {
-    static constexpr int STRIDE = E::template STRIDE<D>, CHUNKS = D / E::CHUNK, DT = D / 32;
+    static constexpr int STRIDE = 2 * D + 16, CHUNKS = D / CHUNK, DT = D / 32;
 };
 
 // 16 bytes from element 0 .. of a row, `have` of them there; zeros behind
@@ -334,8 +294,8 @@ template <typename E, int D> struct Own {
     {
 #pragma unroll
         for (int s = 0; s < Tile<E, D>::CHUNKS; ++s) {
-            typename E::T x[E::CHUNK / 2];
-            load_piece(row, E::CHUNK * s + E::CHUNK / 2 * h, valid, d, vec && d % (E::CHUNK / 2) == 0, x);
+            typename E::T x[CHUNK / 2];
+            load_piece(row, CHUNK * s + CHUNK / 2 * h, valid, d, vec && d % (CHUNK / 2) == 0, x);
             v[s] = E::part(x);
         }
     }
@@ -349,15 +309,15 @@ template <typename E, int D> __device__ __forceinline__ f32x16 product(const cha
     for (int s = 0; s < Tile<E, D>::CHUNKS; ++s) acc = E::rows(p + 32 * s, plane, own.v[s], acc);
     return acc;
 }
-// acc[dt] += (32 streamed rows, transposed) p
-template <typename E, int D>
-__device__ __forceinline__ void fold(const char *tile, int plane, const f32x16 &p, int left, f32x16 (&acc)[Tile<E, D>::DT])
+// acc[dt] += (32 streamed rows, transposed) p, for the channels from `left`'s on
+template <typename E, int D, int N>
+__device__ __forceinline__ void fold(const char *tile, int plane, const f32x16 &p, int left, f32x16 (&acc)[N])
 {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const typename E::Col b = E::col(p, s);
 #pragma unroll
-        for (int dt = 0; dt < Tile<E, D>::DT; ++dt) acc[dt] = E::cols(tile + left, Tile<E, D>::STRIDE, plane, s, dt, b, acc[dt]);
+        for (int dt = 0; dt < N; ++dt) acc[dt] = E::cols(tile + left, Tile<E, D>::STRIDE, plane, s, dt, b, acc[dt]);
     }
 }
 // this lane's row of a result: channel 32 dt + 8 (r / 4) + 4 h + r % 4
@@ -384,11 +344,14 @@ __device__ __forceinline__ void store_row(U *row, const f32x16 (&acc)[DT], float
 // Which of 64 keys from `key` on are there and seen.
 __device__ __forceinline__ int key_byte(const uint8_t *mask, int key, int end) { return key < end ? (mask ? (int)mask[key] : 1) : 0; }
 
-// Sizes of the passes over the keys.  QW wavefronts have rows of their own and KW = WAVES / QW share a row tile's keys:
-// 4 x 1 for long queries, 1 x 4 where a shape has few query rows and the keys are what there is to read.
+// Sizes of the passes over the keys.  QW wavefronts have rows of their own and KW share a row tile's keys: 4 x 1 (wide)
+// where there are rows for every compute unit, 1 x 4 (narrow) where there are few and the keys are most of what there
+// is to read or to wait for.  Where four tiles of keys are too much for LDS, two are shared by two wavefronts
+// each, DW, which form the same scores and half of the result's channels.
 template <typename E, int D, int QW> struct Keys {
-    static constexpr int WAVES = QW == 1 && D * sizeof(typename E::T) > 256 ? 2 : 4, THREADS = 64 * WAVES, KW = WAVES / QW, BQ = 32 * QW;
-    static constexpr int BK = QW == 1 ? 32 * KW : E::PLANES == 1 && sizeof(typename E::T) == 2 ? 64 : 32, NT = BK / 32 / KW;
+    static constexpr int WAVES = 4, THREADS = 64 * WAVES, DW = QW == 1 && E::PLANES == 3 && D > 64 ? 2 : 1, KW = WAVES / QW / DW, BQ = 32 * QW;
+    static constexpr int DT = D / 32 / DW;                  // of a wavefront's result
+    static constexpr int BK = QW == 1 ? 32 * KW : E::PLANES == 1 ? 64 : 32, NT = BK / 32 / KW;
     static constexpr int PLANE = BK * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE;
     static constexpr int BUFFERS = QW == 1 || 4 * TILE > 80 * 1024 ? 1 : 2;     // two where two workgroups still share a compute unit
     static constexpr int WORDS = (BK + 63) / 64;
@@ -408,7 +371,7 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
     typedef typename E::T T;
     __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-    const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave : 0;
+    const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave % S::KW : 0, dw = QW == 1 ? wave / S::KW : 0;
     const int w = work_item(blockIdx.x);
     if (w >= a.total) return;
     const int split = w % a.splits, slot = w / a.splits % a.slots, kvh = w / a.splits / a.slots;
@@ -430,11 +393,11 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
     const uint8_t *mask = a.mask ? a.mask + k.begin : nullptr;
     const int len = k.end - k.begin;
-    const int left = E::left(lane, L::STRIDE);
+    const int left = left16(lane, L::STRIDE) + 64 * S::DT * dw;
 
-    f32x16 acc[L::DT];
+    f32x16 acc[S::DT];
 #pragma unroll
-    for (int dt = 0; dt < L::DT; ++dt) acc[dt] = f32x16{};
+    for (int dt = 0; dt < S::DT; ++dt) acc[dt] = f32x16{};
     float m = -INFINITY, l = 0.f;
 
     Stage<E, D, S::BK, S::THREADS> ks, vs;
@@ -485,7 +448,7 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
             if (up) m = top;
             l *= f;
 #pragma unroll
-            for (int dt = 0; dt < L::DT; ++dt)
+            for (int dt = 0; dt < S::DT; ++dt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[dt][r] *= f;
         }
@@ -504,47 +467,47 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
 
     if constexpr (QW == 1) {                            // the wavefronts' shares of the keys, joined in LDS
         __syncthreads();
-        constexpr int W = D + 4;                        // floats of a row: its sums, then maximum and sum of weights
+        constexpr int W = 32 * S::DT + 4;               // floats of a row: its sums, then maximum and sum of weights
         float *mine = (float *)lds + (wave * 32 + (lane & 31)) * W;
 #pragma unroll
-        for (int dt = 0; dt < L::DT; ++dt)
+        for (int dt = 0; dt < S::DT; ++dt)
 #pragma unroll
             for (int r = 0; r < 16; r += 4)
                 *(f32x4 *)(mine + 32 * dt + reg_row(r) + 4 * h) = f32x4{acc[dt][r], acc[dt][r + 1], acc[dt][r + 2], acc[dt][r + 3]};
-        if (h == 0) { mine[D] = m; mine[D + 1] = l; }
+        if (h == 0) { mine[32 * S::DT] = m; mine[32 * S::DT + 1] = l; }
         __syncthreads();
-        if (wave) return;
+        if (kw) return;
         float f[S::KW];
-        const float *all = (const float *)lds + (lane & 31) * W;
         m = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < S::KW; ++i) m = fmaxf(m, all[i * 32 * W + D]);
+        for (int i = 0; i < S::KW; ++i) m = fmaxf(m, mine[i * 32 * W + 32 * S::DT]);
         l = 0.f;
 #pragma unroll
         for (int i = 0; i < S::KW; ++i) {
-            f[i] = m == -INFINITY ? 0.f : exp2_fast(all[i * 32 * W + D] - m);
-            l += f[i] * all[i * 32 * W + D + 1];
+            f[i] = m == -INFINITY ? 0.f : exp2_fast(mine[i * 32 * W + 32 * S::DT] - m);
+            l += f[i] * mine[i * 32 * W + 32 * S::DT + 1];
         }
 #pragma unroll
-        for (int dt = 0; dt < L::DT; ++dt)
+        for (int dt = 0; dt < S::DT; ++dt)
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < S::KW; ++i) t += f[i] * *(const f32x4 *)(all + i * 32 * W + 32 * dt + reg_row(r) + 4 * h);
+                for (int i = 0; i < S::KW; ++i) t += f[i] * *(const f32x4 *)(mine + i * 32 * W + 32 * dt + reg_row(r) + 4 * h);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[dt][r + j] = t[j];
             }
     }
     if (!valid) return;
     const int64_t at = token * a.hq + head;
+    const int e0 = 32 * S::DT * dw;
     if (a.splits == 1) {
-        store_row<T>((T *)a.Ow + token * a.ld_o + (int64_t)head * a.d, acc, l > 0.f || l != l ? 1.f / l : 0.f, a.d, a.vec, h);
-        if (a.lse && h == 0) a.lse[at] = l > 0.f || l != l ? m * LN2 + logf(l) : -INFINITY;
+        store_row<T>((T *)a.Ow + token * a.ld_o + (int64_t)head * a.d + e0, acc, l > 0.f || l != l ? 1.f / l : 0.f, a.d - e0, a.vec, h);
+        if (a.lse && h == 0 && dw == 0) a.lse[at] = l > 0.f || l != l ? m * LN2 + logf(l) : -INFINITY;
     } else {
         const int64_t p = (int64_t)split * a.nq * a.hq + at;
-        if (l > 0.f || l != l) store_row<float>(a.part + p * a.d, acc, 1.f, a.d, a.d % 4 == 0, h);
-        if (h == 0) a.ml[p] = make_float2(m, l);
+        if (l > 0.f || l != l) store_row<float>(a.part + p * a.d + e0, acc, 1.f, a.d - e0, a.d % 4 == 0, h);
+        if (h == 0 && dw == 0) a.ml[p] = make_float2(m, l);
     }
 }
 
@@ -621,6 +584,31 @@ template <typename T, int D> __device__ __forceinline__ float row_dot(const T *a
     return t + other_half(t);
 }
 
+// acc of the first wavefront = the sum of those of WAVES neighbours, in their order; every wavefront of the workgroup takes part
+template <int DT, int WAVES> __device__ __forceinline__ void join_waves(char *lds, f32x16 (&acc)[DT], int wave, int lane)
+{
+    constexpr int W = 32 * DT + 4;                      // floats of a row; 16 bytes further on each
+    const int h = lane >> 5;
+    float *mine = (float *)lds + (wave * 32 + (lane & 31)) * W + 4 * h;
+    __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) *(f32x4 *)(mine + 32 * dt + reg_row(r)) = f32x4{acc[dt][r], acc[dt][r + 1], acc[dt][r + 2], acc[dt][r + 3]};
+    __syncthreads();
+    if (wave % WAVES) return;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) t += *(const f32x4 *)(mine + i * 32 * W + 32 * dt + reg_row(r));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[dt][r + j] = t[j];
+        }
+}
+
 // dQ, and D for the pass over the keys: the walk of the forward kernel.
 template <typename E, int D, int QW>
 __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(Args a)
@@ -630,7 +618,7 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(
     typedef typename E::T T;
     __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-    const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave : 0;
+    const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave % S::KW : 0, dw = QW == 1 ? wave / S::KW : 0;
     const int w = work_item(blockIdx.x);
     if (w >= a.total) return;
     const int split = w % a.splits, slot = w / a.splits % a.slots, kvh = w / a.splits / a.slots;
@@ -653,18 +641,18 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(
     grad.load((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d, part, a.d, a.vec, h);
     const float delta = row_dot<T, D>((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d,
                                       (const T *)a.O + token * a.ld_o + (int64_t)head * a.d, part, a.d, a.vec, h);
-    if (valid && split == 0 && kw == 0 && h == 0) a.delta[at] = delta;
+    if (valid && split == 0 && kw == 0 && dw == 0 && h == 0) a.delta[at] = delta;
 
     const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
     const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
     const uint8_t *mask = a.mask ? a.mask + k.begin : nullptr;
     const int len = k.end - k.begin;
-    const int left = E::left(lane, L::STRIDE);
+    const int left = left16(lane, L::STRIDE) + 64 * S::DT * dw;
 
-    f32x16 acc[L::DT];
+    f32x16 acc[S::DT];
 #pragma unroll
-    for (int dt = 0; dt < L::DT; ++dt) acc[dt] = f32x16{};
+    for (int dt = 0; dt < S::DT; ++dt) acc[dt] = f32x16{};
     Stage<E, D, S::BK, S::THREADS> ks, vs;
     int seen[S::WORDS];
     auto load = [&](int t) {
@@ -707,31 +695,13 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(
         }
     }
     if constexpr (QW == 1) {
-        __syncthreads();
-        constexpr int W = D + 4;
-        float *mine = (float *)lds + (wave * 32 + (lane & 31)) * W;
-#pragma unroll
-        for (int dt = 0; dt < L::DT; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                *(f32x4 *)(mine + 32 * dt + reg_row(r) + 4 * h) = f32x4{acc[dt][r], acc[dt][r + 1], acc[dt][r + 2], acc[dt][r + 3]};
-        __syncthreads();
-        if (wave) return;
-        const float *all = (const float *)lds + (lane & 31) * W;
-#pragma unroll
-        for (int dt = 0; dt < L::DT; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                f32x4 t = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < S::KW; ++i) t += *(const f32x4 *)(all + i * 32 * W + 32 * dt + reg_row(r) + 4 * h);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[dt][r + j] = t[j];
-            }
+        join_waves<S::DT, S::KW>(lds, acc, wave, lane);
+        if (kw) return;
     }
     if (!valid) return;
-    if (a.splits == 1) store_row<T>((T *)a.dQ + token * a.ld_dq + (int64_t)head * a.d, acc, a.scale, a.d, a.vec, h);
-    else store_row<float>(a.part + ((int64_t)split * a.nq * a.hq + at) * a.d, acc, a.scale, a.d, a.d % 4 == 0, h);
+    const int e0 = 32 * S::DT * dw;
+    if (a.splits == 1) store_row<T>((T *)a.dQ + token * a.ld_dq + (int64_t)head * a.d + e0, acc, a.scale, a.d - e0, a.vec, h);
+    else store_row<float>(a.part + ((int64_t)split * a.nq * a.hq + at) * a.d + e0, acc, a.scale, a.d - e0, a.d % 4 == 0, h);
 }
 
 // dQ = the sum of its splits, in their order; a thread per element
@@ -746,20 +716,24 @@ template <typename T> __global__ __launch_bounds__(256) void attn_bwd_join_kerne
 }
 
 // dK and dV: a wavefront has 32 keys, the queries of all heads that share their head stream past, one head after
-// the other, so the sum over them is taken in registers in a fixed order.
-template <typename E, int D> struct Queries {
-    static constexpr int THREADS = 256, BK = 128, BR = E::PLANES == 1 && sizeof(typename E::T) == 2 ? 64 : 32, NT = BR / 32;
+// the other, so the sum over them is taken in registers in a fixed order.  KW wavefronts have keys of their own (4, wide)
+// or all share 32 keys and deal the queries of a tile among them (1, narrow).
+template <typename E, int D, int KW> struct Queries {
+    static constexpr int WAVES = 4, THREADS = 64 * WAVES, DW = KW == 1 && E::PLANES == 3 && D > 64 ? 2 : 1, QW = WAVES / KW / DW, BK = 32 * KW;
+    static constexpr int DT = D / 32 / DW;
+    static constexpr int BR = KW == 1 ? 32 * QW : E::PLANES == 1 ? 64 : 32, NT = BR / 32 / QW;
     static constexpr int PLANE = BR * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE, BUFFER = 2 * TILE + 2 * BR * 4;
-    static constexpr int BUFFERS = 2 * BUFFER > 80 * 1024 ? 1 : 2, LDS = BUFFERS * BUFFER;
+    static constexpr int BUFFERS = KW == 1 || 2 * BUFFER > 80 * 1024 ? 1 : 2, LDS = BUFFERS * BUFFER;
 };
-template <typename E, int D>
-__global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(Args a)
+template <typename E, int D, int KW>
+__global__ __launch_bounds__((Queries<E, D, KW>::THREADS)) void attn_bwd_dkv_kernel(Args a)
 {
-    typedef Queries<E, D> S;
+    typedef Queries<E, D, KW> S;
     typedef Tile<E, D> L;
     typedef typename E::T T;
     __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int kw = KW == 1 ? 0 : wave, qw = KW == 1 ? wave % S::QW : 0, dw = KW == 1 ? wave / S::QW : 0;
     const int w = work_item(blockIdx.x);
     if (w >= a.total) return;
     const int slot = w % a.slots, kvh = w / a.slots;
@@ -768,17 +742,17 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(Args a)
     const int tile = slot - first_slot(k.begin, 1, S::BK, b);
     if (tile < 0 || tile >= (k.end - k.begin + S::BK - 1) / S::BK) return;
 
-    const int64_t key = k.begin + (int64_t)tile * S::BK + 32 * wave + (lane & 31);
+    const int64_t key = k.begin + (int64_t)tile * S::BK + 32 * kw + (lane & 31);
     const bool valid = key < k.end, seen = valid && (!a.mask || a.mask[key]);
     Own<E, D> kk, vv;
     kk.load((const T *)a.K + (valid ? key : 0) * a.ld_k + (int64_t)kvh * a.d, seen, a.d, a.vec, h);
     vv.load((const T *)a.V + (valid ? key : 0) * a.ld_v + (int64_t)kvh * a.d, seen, a.d, a.vec, h);
 
     const int len = q.end - q.begin, tiles = (len + S::BR - 1) / S::BR, steps = tiles * a.group;
-    const int left = E::left(lane, L::STRIDE);
-    f32x16 dk[L::DT], dv[L::DT];
+    const int left = left16(lane, L::STRIDE) + 64 * S::DT * dw;
+    f32x16 dk[S::DT], dv[S::DT];
 #pragma unroll
-    for (int dt = 0; dt < L::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
+    for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
 
     Stage<E, D, S::BR, S::THREADS> qs, gs;
     float lse = 0.f, delta = 0.f;
@@ -809,31 +783,38 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(Args a)
         if (step + 1 < steps) load(head, t);
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) {
-            f32x16 p = product<E, D>(qt + 32 * i * L::STRIDE, S::PLANE, kk, lane, f32x16{});
+            const int sub = KW == 1 ? qw : i;
+            f32x16 p = product<E, D>(qt + 32 * sub * L::STRIDE, S::PLANE, kk, lane, f32x16{});
             f32x16 g;
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const f32x4 x = *(const f32x4 *)(stat + 32 * i + reg_row(r) + 4 * h);
-                const f32x4 y = *(const f32x4 *)(stat + S::BR + 32 * i + reg_row(r) + 4 * h);
+                const f32x4 x = *(const f32x4 *)(stat + 32 * sub + reg_row(r) + 4 * h);
+                const f32x4 y = *(const f32x4 *)(stat + S::BR + 32 * sub + reg_row(r) + 4 * h);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     p[r + j] = exp2_fast(__builtin_fmaf(p[r + j], a.c, x[j]));
                     g[r + j] = y[j];
                 }
             }
-            g = product<E, D>(gt + 32 * i * L::STRIDE, S::PLANE, vv, lane, g);
-            fold<E, D>(gt + 32 * i * L::STRIDE, S::PLANE, p, left, dv);
+            g = product<E, D>(gt + 32 * sub * L::STRIDE, S::PLANE, vv, lane, g);
+            fold<E, D>(gt + 32 * sub * L::STRIDE, S::PLANE, p, left, dv);
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[r] *= p[r];
-            fold<E, D>(qt + 32 * i * L::STRIDE, S::PLANE, g, left, dk);
+            fold<E, D>(qt + 32 * sub * L::STRIDE, S::PLANE, g, left, dk);
         }
+    }
+    if constexpr (KW == 1) {
+        join_waves<S::DT, S::QW>(lds, dk, wave, lane);
+        join_waves<S::DT, S::QW>(lds, dv, wave, lane);
+        if (qw) return;
     }
     if (!valid) return;
     if (!seen)                                          // a key that is left out: zero, whatever its lane added up
 #pragma unroll
-        for (int dt = 0; dt < L::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
-    store_row<T>((T *)a.dK + key * a.ld_dk + (int64_t)kvh * a.d, dk, a.scale, a.d, a.vec, h);
-    store_row<T>((T *)a.dV + key * a.ld_dv + (int64_t)kvh * a.d, dv, 1.f, a.d, a.vec, h);
+        for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
+    const int e0 = 32 * S::DT * dw;
+    store_row<T>((T *)a.dK + key * a.ld_dk + (int64_t)kvh * a.d + e0, dk, a.scale, a.d - e0, a.vec, h);
+    store_row<T>((T *)a.dV + key * a.ld_dv + (int64_t)kvh * a.d + e0, dv, 1.f, a.d - e0, a.vec, h);
 }
 
 }  // namespace attn

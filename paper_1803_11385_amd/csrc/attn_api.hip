@@ -13,27 +13,39 @@ size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 
 // How a pass over the keys is cut.
 struct Plan {
-    bool few;              // one row tile of 32 per workgroup, whose wavefronts share the keys
-    int bq;
+    bool narrow;           // one row tile of 32 per workgroup, whose wavefronts share the keys
     int64_t slots;
     int splits;
 };
+
+// Workgroups of tiles of `size` rows there will be about (offsets are known on the device only).
+int64_t tiles_of(int64_t rows, int size, int batch, int heads) { return std::max<int64_t>(batch, (rows + size - 1) / size) * heads; }
+
+// The narrow forms take a quarter of the time for a tile, but hold as much of LDS (in fp32 beyond 32 channels all
+// that a compute unit lets two workgroups have) for a quarter of the rows.  They are taken where a single round of them
+// takes all tiles: measured at (wide workgroups) bf16 10: 45 -> 22 us, 38: 8.7 -> 7.2, 170: 27 -> 34; fp32 to 32 channels 52: 17 -> 13,
+// 192: 20 -> 22; beyond 400: 43 -> 107.
+bool narrow_fits(const hch_attn_desc &p, int64_t wide_workgroups)
+{
+    return wide_workgroups <= (p.dtype == HCH_BF16 || p.head_dim <= 32 ? 128 : 64);
+}
 
 Plan plan_keys(const hch_attn_desc &p)
 {
     const int group = p.heads_q / p.heads_kv;
     Plan r;
-    // Rows of a shape (all heads of a key head) that fit one tile of 32: then the keys are most of what there is to read.
-    r.few = p.n_q * group <= (int64_t)32 * p.batch;
-    r.bq = r.few ? 32 : 128;
-    r.slots = hch::attn::slots_of(p.n_q, group, r.bq, p.batch);
-    // Workgroups there will be about, and tiles of keys each has; where the former do not fill the chip (256 compute
-    // units with 4 workgroups of the one form or 2 of the other) the keys are split and the parts joined by a second launch.
-    const int64_t wgs = std::max<int64_t>(p.batch, (p.n_q * group + r.bq - 1) / r.bq) * p.heads_kv;
-    const int64_t tiles = p.n_k / p.batch / (r.few ? 128 : 64), want = r.few ? 1024 : 512;
-    r.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / std::max<int64_t>(1, wgs), tiles / (r.few ? 2 : 4), 256}));
+    r.narrow = p.n_q * group <= (int64_t)32 * p.batch || narrow_fits(p, tiles_of(p.n_q * group, 128, p.batch, p.heads_kv));
+    const int bq = r.narrow ? 32 : 128;
+    r.slots = hch::attn::slots_of(p.n_q, group, bq, p.batch);
+    // Where the workgroups do not fill the chip (256 compute units with 4 or 2 of them), the keys are split among
+    // several and the parts joined by a second launch.
+    const int64_t wgs = tiles_of(p.n_q * group, bq, p.batch, p.heads_kv);
+    const int64_t tiles = p.n_k / p.batch / (r.narrow ? 128 : 64), want = r.narrow ? 1024 : 512;
+    r.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / std::max<int64_t>(1, wgs), tiles / (r.narrow ? 2 : 4), 256}));
     return r;
 }
+
+bool narrow_queries(const hch_attn_desc &p) { return narrow_fits(p, tiles_of(p.n_k, 128, p.batch, p.heads_kv)); }
 
 size_t part_bytes(const hch_attn_desc &p, int splits) { return splits > 1 ? round256((size_t)splits * p.n_q * p.heads_q * p.head_dim * 4) : 0; }
 size_t ml_bytes(const hch_attn_desc &p, int splits) { return splits > 1 ? round256((size_t)splits * p.n_q * p.heads_q * 8) : 0; }
@@ -64,7 +76,7 @@ hch_status check_sizes(const char *who, const hch_attn_desc *p)
     if (p->batch == 0 && (p->n_q || p->n_k)) return fail(HCH_EINVAL, name + ": rows without a shape");
     const int64_t group = p->heads_q / p->heads_kv;
     if (p->batch && (hch::attn::slots_of(p->n_q, (int)group, 32, p->batch) * p->heads_kv * 2 + 1024 > 0x7fffffff ||
-                     hch::attn::slots_of(p->n_k, 1, 128, p->batch) * p->heads_kv + 1024 > 0x7fffffff))
+                     hch::attn::slots_of(p->n_k, 1, 32, p->batch) * p->heads_kv + 1024 > 0x7fffffff))
         return fail(HCH_EUNSUPPORTED, name + ": too many rows for one launch");
     return HCH_OK;
 }
@@ -135,8 +147,8 @@ extern "C" hch_status hch_attn_fwd(const hch_attn_desc *desc, const void *Q, con
     a.part = (float *)workspace;
     a.ml = (float2 *)((char *)workspace + part_bytes(p, r.splits));
     const double bytes = row_bytes(p, 2, 2), flops = 4 * pairs(p);
-    return p.dtype == HCH_F32 ? hch::attn::launch_fwd<float>(a, r.few, bytes, flops, (hipStream_t)stream)
-                              : hch::attn::launch_fwd<__bf16>(a, r.few, bytes, flops, (hipStream_t)stream);
+    return p.dtype == HCH_F32 ? hch::attn::launch_fwd<float>(a, r.narrow, bytes, flops, (hipStream_t)stream)
+                              : hch::attn::launch_fwd<__bf16>(a, r.narrow, bytes, flops, (hipStream_t)stream);
 }
 
 extern "C" hch_status hch_attn_bwd(const hch_attn_desc *desc, const void *Q, const void *K, const void *V, const void *O, const float *lse,
@@ -160,14 +172,16 @@ extern "C" hch_status hch_attn_bwd(const hch_attn_desc *desc, const void *Q, con
         a.delta = (float *)workspace;
         a.part = (float *)((char *)workspace + delta_bytes(p));
         const double bytes = row_bytes(p, 4, 2), flops = 6 * pairs(p);
-        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dq<float>(a, r.few, bytes, flops, s)
-                                : hch::attn::launch_bwd_dq<__bf16>(a, r.few, bytes, flops, s);
+        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dq<float>(a, r.narrow, bytes, flops, s)
+                                : hch::attn::launch_bwd_dq<__bf16>(a, r.narrow, bytes, flops, s);
         if (st != HCH_OK) return st;
     }
     if (p.n_k) {
-        a.slots = (int)hch::attn::slots_of(p.n_k, 1, 128, p.batch); a.splits = 1; a.total = a.slots * a.hkv;
+        const bool narrow = narrow_queries(p);
+        a.slots = (int)hch::attn::slots_of(p.n_k, 1, narrow ? 32 : 128, p.batch); a.splits = 1; a.total = a.slots * a.hkv;
         const double bytes = row_bytes(p, 2, 4), flops = 8 * pairs(p);
-        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dkv<float>(a, bytes, flops, s) : hch::attn::launch_bwd_dkv<__bf16>(a, bytes, flops, s);
+        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dkv<float>(a, narrow, bytes, flops, s)
+                                : hch::attn::launch_bwd_dkv<__bf16>(a, narrow, bytes, flops, s);
     }
     return st;
 }

@@ -7,36 +7,38 @@
 namespace hch {
 namespace attn {
 
-// `few`: the form for few query rows per shape (Keys<T, D, 1>).  flops: of the whole pass, for the profile.
-template <typename T> hch_status launch_fwd(const Args &a, bool few, double bytes, double flops, hipStream_t s);
-template <typename T> hch_status launch_bwd_dq(const Args &a, bool few, double bytes, double flops, hipStream_t s);
-template <typename T> hch_status launch_bwd_dkv(const Args &a, double bytes, double flops, hipStream_t s);
+// `narrow`: one tile of 32 rows (keys) per workgroup (Keys<E, D, 1>, Queries<E, D, 1>).  flops: of the whole pass, for the profile.
+template <typename T> hch_status launch_fwd(const Args &a, bool narrow, double bytes, double flops, hipStream_t s);
+template <typename T> hch_status launch_bwd_dq(const Args &a, bool narrow, double bytes, double flops, hipStream_t s);
+template <typename T> hch_status launch_bwd_dkv(const Args &a, bool narrow, double bytes, double flops, hipStream_t s);
 
 #ifdef HCH_ATTN_TYPE
-// The engines of a type: for passes that the products bound, and for the form for few queries, which memory bounds.
-template <typename T> struct Engine { typedef Bf16 Many, Few; };
-template <> struct Engine<float> { typedef Split Many; typedef Fp32 Few; };
+template <typename T> struct EngineOf { typedef Bf16 E; };
+template <> struct EngineOf<float> { typedef Split E; };
 
-template <typename F> void with_width(int d, F &&f)
+// The instance for heads of d channels.  fp32's narrow forms share a result's channels between two wavefronts beyond 64: no 96.
+template <typename T, typename F> void with_width(int d, bool narrow, F &&f)
 {
     if (d <= 32) f(std::integral_constant<int, 32>{});
     else if (d <= 64) f(std::integral_constant<int, 64>{});
-    else if (d <= 96) f(std::integral_constant<int, 96>{});
+    else if (d <= 96 && !(narrow && sizeof(T) == 4)) f(std::integral_constant<int, 96>{});
     else f(std::integral_constant<int, 128>{});
 }
+template <typename T, int D> constexpr bool has_narrow = sizeof(T) == 2 || D != 96;
 
-template <typename T> hch_status launch_fwd(const Args &a, bool few, double bytes, double flops, hipStream_t s)
+template <typename T> hch_status launch_fwd(const Args &a, bool narrow, double bytes, double flops, hipStream_t s)
 {
     {
         LaunchTimer lt(HCH_KERNEL_ID("attn_fwd_kernel"), s, bytes, flops);
-        with_width(a.d, [&](auto w) {
+        with_width<T>(a.d, narrow, [&](auto w) {
+            typedef typename EngineOf<T>::E E;
             constexpr int D = decltype(w)::value;
-            if (few) {
-                constexpr auto kernel = attn_fwd_kernel<typename Engine<T>::Few, D, 1>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<typename Engine<T>::Few, D, 1>::THREADS)), 0, s, a);
-            } else {
-                constexpr auto kernel = attn_fwd_kernel<typename Engine<T>::Many, D, 4>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<typename Engine<T>::Many, D, 4>::THREADS)), 0, s, a);
+            if (!narrow) {
+                constexpr auto kernel = attn_fwd_kernel<E, D, 4>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 4>::THREADS)), 0, s, a);
+            } else if constexpr (has_narrow<T, D>) {
+                constexpr auto kernel = attn_fwd_kernel<E, D, 1>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 1>::THREADS)), 0, s, a);
             }
         });
     }
@@ -55,18 +57,19 @@ template <typename T> hch_status launch_fwd(const Args &a, bool few, double byte
     return HCH_OK;
 }
 
-template <typename T> hch_status launch_bwd_dq(const Args &a, bool few, double bytes, double flops, hipStream_t s)
+template <typename T> hch_status launch_bwd_dq(const Args &a, bool narrow, double bytes, double flops, hipStream_t s)
 {
     {
         LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_dq_kernel"), s, bytes, flops);
-        with_width(a.d, [&](auto w) {
+        with_width<T>(a.d, narrow, [&](auto w) {
+            typedef typename EngineOf<T>::E E;
             constexpr int D = decltype(w)::value;
-            if (few) {
-                constexpr auto kernel = attn_bwd_dq_kernel<typename Engine<T>::Few, D, 1>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<typename Engine<T>::Few, D, 1>::THREADS)), 0, s, a);
-            } else {
-                constexpr auto kernel = attn_bwd_dq_kernel<typename Engine<T>::Many, D, 4>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<typename Engine<T>::Many, D, 4>::THREADS)), 0, s, a);
+            if (!narrow) {
+                constexpr auto kernel = attn_bwd_dq_kernel<E, D, 4>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 4>::THREADS)), 0, s, a);
+            } else if constexpr (has_narrow<T, D>) {
+                constexpr auto kernel = attn_bwd_dq_kernel<E, D, 1>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 1>::THREADS)), 0, s, a);
             }
         });
     }
@@ -82,13 +85,20 @@ template <typename T> hch_status launch_bwd_dq(const Args &a, bool few, double b
     return HCH_OK;
 }
 
-template <typename T> hch_status launch_bwd_dkv(const Args &a, double bytes, double flops, hipStream_t s)
+template <typename T> hch_status launch_bwd_dkv(const Args &a, bool narrow, double bytes, double flops, hipStream_t s)
 {
     {
         LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_dkv_kernel"), s, bytes, flops);
-        with_width(a.d, [&](auto w) {
-            constexpr auto kernel = attn_bwd_dkv_kernel<typename Engine<T>::Many, decltype(w)::value>;
-            HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3(256), 0, s, a);
+        with_width<T>(a.d, narrow, [&](auto w) {
+            typedef typename EngineOf<T>::E E;
+            constexpr int D = decltype(w)::value;
+            if (!narrow) {
+                constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 4>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Queries<E, D, 4>::THREADS)), 0, s, a);
+            } else if constexpr (has_narrow<T, D>) {
+                constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 1>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Queries<E, D, 1>::THREADS)), 0, s, a);
+            }
         });
     }
     HCH_LAUNCH_CHECK("attn_bwd_dkv_kernel");
@@ -97,7 +107,7 @@ template <typename T> hch_status launch_bwd_dkv(const Args &a, double bytes, dou
 
 template hch_status launch_fwd<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
 template hch_status launch_bwd_dq<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
-template hch_status launch_bwd_dkv<HCH_ATTN_TYPE>(const Args &, double, double, hipStream_t);
+template hch_status launch_bwd_dkv<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
 #endif
 
 }  // namespace attn
