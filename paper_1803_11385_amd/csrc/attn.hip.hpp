@@ -12,8 +12,8 @@
 //   * the probabilities are already laid out as the right operand of the second product, whose reduction runs
 //     over the streamed rows: register r of half h is row 8 (r / 4) + 4 h + r % 4, and the left operand is read
 //     in the same order, so nothing is exchanged between the products.
-// The streamed tile lies row by row in LDS, 16 bytes between rows: ds_read_b128 for products over the channels
-// (16 consecutive bytes of a row), for products over the rows the transposing ds_read_b64_tr_b16 (16 lanes give the
+// The streamed tile lies row by row in LDS and serves both: ds_read_b128 for products over the channels (16
+// consecutive bytes of a row), for products over the rows the transposing ds_read_b64_tr_b16 (16 lanes give the
 // addresses of 4 rows x 16 channels and get 4 rows of one channel each).
 #pragma once
 #include <hip/hip_runtime.h>
@@ -60,16 +60,37 @@ struct Args {
 //   cols   acc += (16 streamed rows of the tile, transposed) col, channels 32 dt ..
 constexpr int CHUNK = 16;
 
-// a transposed piece of 16 rows x 32 channels, 16-bit elements; p: the tile's rows 16 s, channels 32 dt, with this
-// lane's offset left16
-__device__ __forceinline__ int left16(int lane, int stride)
+// A tile's rows lie one after the other, their 16-byte units swapped: unit u of row r at u ^ swap(r), so that neither
+// product's reads meet in a bank (LDS has 64 of 4 bytes).  ds_read_b128 of one unit of 32 rows serves 16 lanes a
+// clock whose rows differ modulo 16: these have to spread over the 16 units that the banks hold.  The transposing read
+// serves 4 rows x 4 neighbouring units a clock: the rows' groups of 4 units have to differ.  (With 16 bytes between the rows
+// instead, the second kind took twice (64 channels) to four times (128) as long.)
+template <int D> struct Layout {
+    static constexpr int STRIDE = 2 * D;
+    static __device__ __forceinline__ int swap(int r)
+    {
+        return (r >> 2 & 3) | (D == 128 ? (r & 3) << 2 : D == 64 ? (r >> 1 & 1) << 2 : 0);
+    }
+    // offset of this lane's row of 32, unit 16 s + 8 h channels, of a product over the channels: from the s = 0 one
+    static __device__ __forceinline__ int row0(int lane) { const int r = lane & 31; return r * STRIDE + (((lane >> 5) ^ swap(r)) << 4); }
+    static __device__ __forceinline__ int row(int at, int s)
+    {
+        constexpr int X = D == 128 ? 7 : D == 64 ? 3 : 1;      // what of s lies within the units that are swapped
+        return (at ^ (s & X) << 5) + ((s & ~X) << 5);
+    }
+    // offset of this lane's address in the transposing read of rows 0 .. 3 and 4 .. 7 (by half), channels 0 .. 31
+    static __device__ __forceinline__ int left0(int lane)
+    {
+        const int r = 4 * (lane >> 5) + ((lane & 15) >> 2), u = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+        return r * STRIDE + ((u ^ swap(r)) << 4) + 8 * (lane & 1);
+    }
+    static __device__ __forceinline__ int left(int at, int dt) { return D == 96 ? at + (dt << 6) : at ^ dt << 6; }
+};
+// 16 streamed rows x 32 channels, transposed: row 4 h + j and 8 + 4 h + j of channel lane % 32
+template <int D> __device__ __forceinline__ bf16x8 transposed(const char *rows16, int at)
 {
-    return (4 * (lane >> 5) + ((lane & 15) >> 2)) * stride + (16 * ((lane >> 4) & 1) + (lane & 3) * 4) * 2;
-}
-__device__ __forceinline__ bf16x8 transposed(const char *p, int stride)
-{
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)p);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)(p + 8 * stride));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)(rows16 + at));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s16x4 *)(rows16 + 8 * Layout<D>::STRIDE + (at ^ 32)));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 __device__ __forceinline__ f32x16 mfma16(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -88,11 +109,12 @@ struct Bf16 {
         for (int j = 0; j < 8; ++j) c[j] = (__bf16)p[8 * s + j];
         return c;
     }
-    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int, int s, int dt, const Col &b, f32x16 acc)
+    template <int D> static __device__ __forceinline__ f32x16 cols(const char *rows16, int, int at, const Col &b, f32x16 acc)
     {
-        return mfma16(transposed(tile + 16 * s * stride + 64 * dt, stride), b, acc);
+        return mfma16(transposed<D>(rows16, at), b, acc);
     }
-    static __device__ __forceinline__ void store(char *row, int, int piece, u32x4 v) { *(u32x4 *)(row + 16 * piece) = v; }
+    // 16 bytes of memory into a row whose units are swapped by `swap`
+    static __device__ __forceinline__ void store(char *row, int, int swap, int piece, u32x4 v) { *(u32x4 *)(row + 16 * (piece ^ swap)) = v; }
 };
 
 // fp32 on the bf16 instruction: every number is the sum of three bf16 numbers (8 bits each, so exact), and of the nine
@@ -149,13 +171,12 @@ struct Split {
         const float x[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
         return part(x);
     }
-    static __device__ __forceinline__ f32x16 cols(const char *tile, int stride, int plane, int s, int dt, const Col &b, f32x16 acc)
+    template <int D> static __device__ __forceinline__ f32x16 cols(const char *rows16, int plane, int at, const Col &b, f32x16 acc)
     {
-        const char *p = tile + 16 * s * stride + 64 * dt;
-        const bf16x8 a[3] = {transposed(p, stride), transposed(p + plane, stride), transposed(p + 2 * plane, stride)};
+        const bf16x8 a[3] = {transposed<D>(rows16, at), transposed<D>(rows16 + plane, at), transposed<D>(rows16 + 2 * plane, at)};
         return six(a, b.v, acc);
     }
-    static __device__ __forceinline__ void store(char *row, int plane, int piece, u32x4 v)
+    static __device__ __forceinline__ void store(char *row, int plane, int swap, int piece, u32x4 v)
     {
         const f32x4 x = __builtin_bit_cast(f32x4, v);
         uint32_t lo[3], hi[3];
@@ -163,7 +184,7 @@ struct Split {
         cut(x[2], x[3], hi);
         typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int k = 0; k < 3; ++k) *(u32x2 *)(row + k * plane + 8 * piece) = u32x2{lo[k], hi[k]};
+        for (int k = 0; k < 3; ++k) *(u32x2 *)(row + k * plane + 8 * (piece ^ 2 * swap)) = u32x2{lo[k], hi[k]};
     }
 };
 
@@ -220,7 +241,7 @@ inline int64_t slots_of(int64_t n, int rows_each, int size, int batch) { return 
 // tiles
 // ---------------------------------------------------------------------------------------------
 template <typename E, int D> struct Tile {
-    static constexpr int STRIDE = 2 * D + 16, CHUNKS = D / CHUNK, DT = D / 32;
+    static constexpr int STRIDE = Layout<D>::STRIDE, CHUNKS = D / CHUNK, DT = D / 32;
 };
 
 // 16 bytes from element 0 .. of a row, `have` of them there; zeros behind
@@ -271,7 +292,7 @@ template <typename E, int D, int ROWS, int THREADS> struct Stage {
             if (PIECES % THREADS && p >= PIECES) continue;
             u32x4 v = r[i];
             if (keep && !(keep[row >> 6] >> (row & 63) & 1)) v = u32x4{0, 0, 0, 0};
-            E::store(tile + row * Tile<E, D>::STRIDE, ROWS * Tile<E, D>::STRIDE, col, v);
+            E::store(tile + row * Tile<E, D>::STRIDE, ROWS * Tile<E, D>::STRIDE, Layout<D>::swap(row), col, v);
         }
     }
 };
@@ -304,9 +325,9 @@ template <typename E, int D> struct Own {
 // scores of 32 streamed rows against the own rows; plane: bytes between the planes of the tile
 template <typename E, int D> __device__ __forceinline__ f32x16 product(const char *tile, int plane, const Own<E, D> &own, int lane, f32x16 acc)
 {
-    const char *p = tile + (lane & 31) * Tile<E, D>::STRIDE + 16 * (lane >> 5);       // a chunk is 32 bytes of a plane
+    const int at = Layout<D>::row0(lane);
 #pragma unroll
-    for (int s = 0; s < Tile<E, D>::CHUNKS; ++s) acc = E::rows(p + 32 * s, plane, own.v[s], acc);
+    for (int s = 0; s < Tile<E, D>::CHUNKS; ++s) acc = E::rows(tile + Layout<D>::row(at, s), plane, own.v[s], acc);
     return acc;
 }
 // acc[dt] += (32 streamed rows, transposed) p, for the channels from `left`'s on
@@ -317,7 +338,8 @@ __device__ __forceinline__ void fold(const char *tile, int plane, const f32x16 &
     for (int s = 0; s < 2; ++s) {
         const typename E::Col b = E::col(p, s);
 #pragma unroll
-        for (int dt = 0; dt < N; ++dt) acc[dt] = E::cols(tile + left, Tile<E, D>::STRIDE, plane, s, dt, b, acc[dt]);
+        for (int dt = 0; dt < N; ++dt)
+            acc[dt] = E::template cols<D>(tile + 16 * s * Tile<E, D>::STRIDE, plane, Layout<D>::left(left, dt), b, acc[dt]);
     }
 }
 // this lane's row of a result: channel 32 dt + 8 (r / 4) + 4 h + r % 4
@@ -355,7 +377,7 @@ template <typename E, int D, int QW> struct Keys {
     static constexpr int PLANE = BK * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE;
     static constexpr int BUFFERS = QW == 1 || 4 * TILE > 80 * 1024 ? 1 : 2;     // two where two workgroups still share a compute unit
     static constexpr int WORDS = (BK + 63) / 64;
-    static constexpr int LDS = 2 * BUFFERS * TILE;
+    static constexpr int JOIN = QW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = 2 * BUFFERS * TILE > JOIN ? 2 * BUFFERS * TILE : JOIN;
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -393,7 +415,7 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
     const uint8_t *mask = a.mask ? a.mask + k.begin : nullptr;
     const int len = k.end - k.begin;
-    const int left = left16(lane, L::STRIDE) + 64 * S::DT * dw;
+    const int left = Layout<D>::left(Layout<D>::left0(lane), S::DT * dw);
 
     f32x16 acc[S::DT];
 #pragma unroll
@@ -648,7 +670,7 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
     const uint8_t *mask = a.mask ? a.mask + k.begin : nullptr;
     const int len = k.end - k.begin;
-    const int left = left16(lane, L::STRIDE) + 64 * S::DT * dw;
+    const int left = Layout<D>::left(Layout<D>::left0(lane), S::DT * dw);
 
     f32x16 acc[S::DT];
 #pragma unroll
@@ -723,7 +745,8 @@ template <typename E, int D, int KW> struct Queries {
     static constexpr int DT = D / 32 / DW;
     static constexpr int BR = KW == 1 ? 32 * QW : E::PLANES == 1 ? 64 : 32, NT = BR / 32 / QW;
     static constexpr int PLANE = BR * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE, BUFFER = 2 * TILE + 2 * BR * 4;
-    static constexpr int BUFFERS = KW == 1 || 2 * BUFFER > 80 * 1024 ? 1 : 2, LDS = BUFFERS * BUFFER;
+    static constexpr int BUFFERS = KW == 1 || 2 * BUFFER > 80 * 1024 ? 1 : 2;
+    static constexpr int JOIN = KW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = BUFFERS * BUFFER > JOIN ? BUFFERS * BUFFER : JOIN;
 };
 template <typename E, int D, int KW>
 __global__ __launch_bounds__((Queries<E, D, KW>::THREADS)) void attn_bwd_dkv_kernel(Args a)
@@ -749,7 +772,7 @@ __global__ __launch_bounds__((Queries<E, D, KW>::THREADS)) void attn_bwd_dkv_ker
     vv.load((const T *)a.V + (valid ? key : 0) * a.ld_v + (int64_t)kvh * a.d, seen, a.d, a.vec, h);
 
     const int len = q.end - q.begin, tiles = (len + S::BR - 1) / S::BR, steps = tiles * a.group;
-    const int left = left16(lane, L::STRIDE) + 64 * S::DT * dw;
+    const int left = Layout<D>::left(Layout<D>::left0(lane), S::DT * dw);
     f32x16 dk[S::DT], dv[S::DT];
 #pragma unroll
     for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
