@@ -30,6 +30,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr int SRD3 = 0x00020000, OUT = 0x7fffffff;      // raw buffer descriptor; an offset past every buffer
@@ -53,11 +54,12 @@ struct Args {
 // ---------------------------------------------------------------------------------------------
 // how operands are multiplied
 // ---------------------------------------------------------------------------------------------
-// An engine E: T is the type in memory, Part one lane's share of a chunk of 16 channels, PLANES the parts a tile has in
-// LDS.
-//   rows   acc += A B over the channels of a chunk; A from the tile, B the lane's own
-//   col    16 streamed rows of the right operand, registers 8 s .. 8 s + 7 of a tile
-//   cols   acc += (16 streamed rows of the tile, transposed) col, channels 32 dt ..
+// An engine E: T is the type in memory, Part one lane's share of 16 terms of an operand, PLANES the parts a tile has in
+// LDS, AHEAD the operands of a product over the channels that are read before the first is multiplied.
+//   rows   from a tile: 32 rows, 16 channels
+//   cols   from a tile, transposed: 32 channels, 16 rows
+//   col    from a product's result: its registers 8 s .. 8 s + 7, 16 streamed rows
+//   mul    acc += a b
 constexpr int CHUNK = 16;
 
 // A tile's rows lie one after the other, their 16-byte units swapped: unit u of row r at u ^ swap(r), so that neither
@@ -97,22 +99,19 @@ __device__ __forceinline__ f32x16 mfma16(bf16x8 a, bf16x8 b, f32x16 c) { return 
 
 struct Bf16 {
     typedef __bf16 T;
-    static constexpr int PLANES = 1;
+    static constexpr int PLANES = 1, AHEAD = 4;
     typedef bf16x8 Part;
     static __device__ __forceinline__ Part part(const __bf16 (&x)[8]) { return __builtin_bit_cast(bf16x8, x); }
-    static __device__ __forceinline__ f32x16 rows(const char *p, int, const Part &b, f32x16 acc) { return mfma16(*(const bf16x8 *)p, b, acc); }
-    typedef bf16x8 Col;
-    static __device__ __forceinline__ Col col(const f32x16 &p, int s)
+    static __device__ __forceinline__ Part rows(const char *p, int) { return *(const bf16x8 *)p; }
+    template <int D> static __device__ __forceinline__ Part cols(const char *rows16, int, int at) { return transposed<D>(rows16, at); }
+    static __device__ __forceinline__ Part col(const f32x16 &p, int s)
     {
-        Col c;
+        Part c;
 #pragma unroll
         for (int j = 0; j < 8; ++j) c[j] = (__bf16)p[8 * s + j];
         return c;
     }
-    template <int D> static __device__ __forceinline__ f32x16 cols(const char *rows16, int, int at, const Col &b, f32x16 acc)
-    {
-        return mfma16(transposed<D>(rows16, at), b, acc);
-    }
+    static __device__ __forceinline__ f32x16 mul(const Part &a, const Part &b, f32x16 acc) { return mfma16(a, b, acc); }
     // 16 bytes of memory into a row whose units are swapped by `swap`
     static __device__ __forceinline__ void store(char *row, int, int swap, int piece, u32x4 v) { *(u32x4 *)(row + 16 * (piece ^ swap)) = v; }
 };
@@ -123,9 +122,8 @@ struct Bf16 {
 // are lost one by one as they fall below 2^-133; an infinite operand makes its sums NaN.)
 struct Split {
     typedef float T;
-    static constexpr int PLANES = 3;
+    static constexpr int PLANES = 3, AHEAD = 1;
     struct Part { bf16x8 v[3]; };
-    typedef Part Col;
     static __device__ __forceinline__ uint32_t round2(float a, float b)
     {
         typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -154,27 +152,25 @@ struct Split {
         for (int k = 0; k < 3; ++k) p.v[k] = __builtin_bit_cast(bf16x8, t[k]);
         return p;
     }
-    static __device__ __forceinline__ f32x16 six(const bf16x8 (&a)[3], const bf16x8 (&b)[3], f32x16 acc)
+    static __device__ __forceinline__ Part rows(const char *p, int plane)
     {
-        constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};      // the smallest first
-#pragma unroll
-        for (int i = 0; i < 6; ++i) acc = mfma16(a[PA[i]], b[PB[i]], acc);
-        return acc;
+        return Part{{*(const bf16x8 *)p, *(const bf16x8 *)(p + plane), *(const bf16x8 *)(p + 2 * plane)}};
     }
-    static __device__ __forceinline__ f32x16 rows(const char *p, int plane, const Part &b, f32x16 acc)
+    template <int D> static __device__ __forceinline__ Part cols(const char *rows16, int plane, int at)
     {
-        const bf16x8 a[3] = {*(const bf16x8 *)p, *(const bf16x8 *)(p + plane), *(const bf16x8 *)(p + 2 * plane)};
-        return six(a, b.v, acc);
+        return Part{{transposed<D>(rows16, at), transposed<D>(rows16 + plane, at), transposed<D>(rows16 + 2 * plane, at)}};
     }
-    static __device__ __forceinline__ Col col(const f32x16 &p, int s)
+    static __device__ __forceinline__ Part col(const f32x16 &p, int s)
     {
         const float x[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
         return part(x);
     }
-    template <int D> static __device__ __forceinline__ f32x16 cols(const char *rows16, int plane, int at, const Col &b, f32x16 acc)
+    static __device__ __forceinline__ f32x16 mul(const Part &a, const Part &b, f32x16 acc)
     {
-        const bf16x8 a[3] = {transposed<D>(rows16, at), transposed<D>(rows16 + plane, at), transposed<D>(rows16 + 2 * plane, at)};
-        return six(a, b.v, acc);
+        constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};      // the smallest first
+#pragma unroll
+        for (int i = 0; i < 6; ++i) acc = mfma16(a.v[PA[i]], b.v[PB[i]], acc);
+        return acc;
     }
     static __device__ __forceinline__ void store(char *row, int plane, int swap, int piece, u32x4 v)
     {
@@ -297,6 +293,48 @@ template <typename E, int D, int ROWS, int THREADS> struct Stage {
     }
 };
 
+// The same without registers, for bf16 in whole pieces: every instruction moves 64 pieces from memory to 1 KB of LDS,
+// lane by lane.  As the place in LDS is the lane's, the swap of the units is in the lane's address in memory.
+template <int D, int ROWS> struct Direct {
+    static constexpr int PER_ROW = D / 8, N = ROWS * PER_ROW / 256;
+    static __device__ __forceinline__ void piece(int i, int wave, int lane, int &row, int &e)
+    {
+        const int p = (wave + 4 * i) * 64 + lane;
+        row = p / PER_ROW;
+        e = ((p - row * PER_ROW) ^ Layout<D>::swap(row)) * 8;
+    }
+    static __device__ __forceinline__ void load(const __bf16 *base, int64_t ld, int row0, int end, int d, char *tile, int wave, int lane)
+    {
+        const int rows = max(0, min(ROWS, end - row0));
+        const int bytes = rows ? (int)(((rows - 1) * ld + d) * 2) : 0;
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(base + row0 * ld), 0, bytes, SRD3);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            int row, e;
+            piece(i, wave, lane, row, e);
+            to_lds(rs, e < d ? (int)(row * ld + e) * 2 : OUT, tile + (wave + 4 * i) * 1024);
+        }
+    }
+    // Written out, as the compiler would wait for all of them before the next transposing read of any part of LDS; that
+    // they have arrived is waited for in wait().  m0: where in LDS lane 0's piece goes.
+    static __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t rs, int offset, char *to)
+    {
+        const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void *)(void *)to);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(m0), "v"(offset), "s"(rs) : "memory");
+    }
+    static __device__ __forceinline__ void clear(char *tile, int wave, int lane, uint64_t keep)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            int row, e;
+            piece(i, wave, lane, row, e);
+            if (!(keep >> row & 1)) *(u32x4 *)(tile + (wave + 4 * i) * 1024 + 16 * lane) = u32x4{0, 0, 0, 0};
+        }
+    }
+    // this wavefront's loads have arrived
+    static __device__ __forceinline__ void wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+};
+
 // `count` elements of a row from element e on; zeros where there are none
 template <typename T, int N> __device__ __forceinline__ void load_piece(const T *row, int e, bool valid, int d, bool vec, T (&x)[N])
 {
@@ -322,26 +360,67 @@ template <typename E, int D> struct Own {
     }
 };
 
-// scores of 32 streamed rows against the own rows; plane: bytes between the planes of the tile
-template <typename E, int D> __device__ __forceinline__ f32x16 product(const char *tile, int plane, const Own<E, D> &own, int lane, f32x16 acc)
-{
-    const int at = Layout<D>::row0(lane);
-#pragma unroll
-    for (int s = 0; s < Tile<E, D>::CHUNKS; ++s) acc = E::rows(tile + Layout<D>::row(at, s), plane, own.v[s], acc);
-    return acc;
-}
-// acc[dt] += (32 streamed rows, transposed) p, for the channels from `left`'s on
+// Nothing but arithmetic other than products moves across: the compiler would read every operand from LDS right before
+// the product that takes it, and wait for it.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x406); }
+
+// out[i] += (rows 32 i .. of the tile) . own, for N runs of 32 rows.  AHEAD operands are read before the first product, and as
+// many more while those multiply.
 template <typename E, int D, int N>
-__device__ __forceinline__ void fold(const char *tile, int plane, const f32x16 &p, int left, f32x16 (&acc)[N])
+__device__ __forceinline__ void products(const char *tile, int plane, const Own<E, D> &own, int lane, f32x16 (&out)[N])
 {
+    constexpr int CH = Tile<E, D>::CHUNKS, G = E::AHEAD, TOTAL = N * CH;
+    const int at = Layout<D>::row0(lane);
+    typename E::Part a[2][G];
+    auto read = [&](int g) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const typename E::Col b = E::col(p, s);
+        for (int i = 0; i < G; ++i)
+            if (g * G + i < TOTAL) a[g & 1][i] = E::rows(tile + 32 * ((g * G + i) / CH) * Tile<E, D>::STRIDE + Layout<D>::row(at, (g * G + i) % CH), plane);
+    };
+    read(0);
 #pragma unroll
-        for (int dt = 0; dt < N; ++dt)
-            acc[dt] = E::template cols<D>(tile + 16 * s * Tile<E, D>::STRIDE, plane, Layout<D>::left(left, dt), b, acc[dt]);
+    for (int g = 0; g * G < TOTAL; ++g) {
+        if ((g + 1) * G < TOTAL) read(g + 1);
+        keep_order();
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+            if (g * G + i < TOTAL) {
+                const int n = (g * G + i) / CH, c = (g * G + i) % CH;
+                out[n] = E::mul(a[g & 1][i], own.v[c], out[n]);
+            }
+        keep_order();
     }
 }
+
+// acc[dt] += (rows of a tile, transposed) p, for the channels from `left`'s on, 16 rows at a time.  The first 16 rows' operands
+// are read by the constructor, so that they arrive while p is still being made.
+template <typename E, int D, int DT> struct Fold {
+    typename E::Part a[2][DT];
+    const char *tile;
+    int plane, left;
+    __device__ __forceinline__ void read(int step)
+    {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) a[step & 1][dt] = E::template cols<D>(tile + 16 * step * Tile<E, D>::STRIDE, plane, Layout<D>::left(left, dt));
+    }
+    __device__ __forceinline__ Fold(const char *t, int pl, int l) : tile(t), plane(pl), left(l)
+    {
+        read(0);
+        keep_order();
+    }
+    template <int N> __device__ __forceinline__ void run(const f32x16 (&p)[N], f32x16 (&acc)[DT])
+    {
+#pragma unroll
+        for (int step = 0; step < 2 * N; ++step) {
+            if (step + 1 < 2 * N) read(step + 1);
+            keep_order();
+            const typename E::Part b = E::col(p[step >> 1], step & 1);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) acc[dt] = E::mul(a[step & 1][dt], b, acc[dt]);
+            keep_order();
+        }
+    }
+};
 // this lane's row of a result: channel 32 dt + 8 (r / 4) + 4 h + r % 4
 template <typename U, int DT>
 __device__ __forceinline__ void store_row(U *row, const f32x16 (&acc)[DT], float f, int d, bool vec, int h)
@@ -370,13 +449,14 @@ __device__ __forceinline__ int key_byte(const uint8_t *mask, int key, int end) {
 // where there are rows for every compute unit, 1 x 4 (narrow) where there are few and the keys are most of what there
 // is to read or to wait for.  Where four tiles of keys are too much for LDS, two are shared by two wavefronts
 // each, DW, which form the same scores and half of the result's channels.
-template <typename E, int D, int QW> struct Keys {
+template <typename E, int D, int QW, bool VEC> struct Keys {
     static constexpr int WAVES = 4, THREADS = 64 * WAVES, DW = QW == 1 && E::PLANES == 3 && D > 64 ? 2 : 1, KW = WAVES / QW / DW, BQ = 32 * QW;
     static constexpr int DT = D / 32 / DW;                  // of a wavefront's result
     static constexpr int BK = QW == 1 ? 32 * KW : E::PLANES == 1 ? 64 : 32, NT = BK / 32 / KW;
     static constexpr int PLANE = BK * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE;
     static constexpr int BUFFERS = QW == 1 || 4 * TILE > 80 * 1024 ? 1 : 2;     // two where two workgroups still share a compute unit
     static constexpr int WORDS = (BK + 63) / 64;
+    static constexpr bool DIRECT = VEC && E::PLANES == 1 && QW == 4;   // two buffers, so the loads of the next tile need no registers
     static constexpr int JOIN = QW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = 2 * BUFFERS * TILE > JOIN ? 2 * BUFFERS * TILE : JOIN;
 };
 
@@ -385,10 +465,10 @@ template <typename E, int D, int QW> struct Keys {
 // ---------------------------------------------------------------------------------------------
 // Query rows of the heads that share a key head are one list, row = token * group + (head within the group), so that
 // a tile of keys serves the whole group.
-template <typename E, int D, int QW>
-__global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Args a)
+template <typename E, int D, int QW, bool VEC>
+__global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::DIRECT ? 2 : 1)) void attn_fwd_kernel(Args a)
 {
-    typedef Keys<E, D, QW> S;
+    typedef Keys<E, D, QW, VEC> S;
     typedef Tile<E, D> L;
     typedef typename E::T T;
     __shared__ __align__(16) char lds[S::LDS];
@@ -408,7 +488,7 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
     const int64_t token = valid ? q.begin + row / a.group : q.begin;
     const int head = kvh * a.group + (valid ? (int)(row % a.group) : 0);
     Own<E, D> own;
-    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, valid, a.d, a.vec, h);
+    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, valid, a.d, VEC, h);
 
     const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
     const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
@@ -422,17 +502,42 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
     for (int dt = 0; dt < S::DT; ++dt) acc[dt] = f32x16{};
     float m = -INFINITY, l = 0.f;
 
-    Stage<E, D, S::BK, S::THREADS> ks, vs;
+    // The next tile is on its way while this one is multiplied: in registers, or straight to the other buffer.
+    typedef Stage<E, D, S::BK, S::THREADS> Regs;
+    typedef Direct<D, S::BK> Dir;
+    Regs ks, vs;
     int seen[S::WORDS];
+    auto buffer = [&](int t) { return lds + (S::BUFFERS == 2 ? (t & 1) * 2 * S::TILE : 0); };
     auto load = [&](int t) {
-        ks.load(kp, a.ld_k, t * S::BK, len, a.d, a.vec, tid);
-        vs.load(vp, a.ld_v, t * S::BK, len, a.d, a.vec, tid);
+        if constexpr (S::DIRECT) {
+            Dir::load(kp, a.ld_k, t * S::BK, len, a.d, buffer(t), wave, lane);
+            Dir::load(vp, a.ld_v, t * S::BK, len, a.d, buffer(t) + S::TILE, wave, lane);
+        } else {
+            ks.load(kp, a.ld_k, t * S::BK, len, a.d, VEC, tid);
+            vs.load(vp, a.ld_v, t * S::BK, len, a.d, VEC, tid);
+        }
 #pragma unroll
         for (int i = 0; i < S::WORDS; ++i) seen[i] = key_byte(mask, t * S::BK + 64 * i + lane, len);
     };
+    // tile t in LDS; keys that are not seen as zeros in the second matrix (0 * NaN), and where asked for in the first
+    auto arrive = [&](int t, const uint64_t *keep, bool all, bool both) {
+        char *kt = buffer(t), *vt = kt + S::TILE;
+        if constexpr (S::DIRECT) {
+            Dir::wait();
+            if (!all) {
+                Dir::clear(vt, wave, lane, keep[0]);
+                if (both) Dir::clear(kt, wave, lane, keep[0]);
+            }
+        } else {
+            if (S::BUFFERS == 1) __syncthreads();
+            ks.store(kt, tid, all || !both ? nullptr : keep);
+            vs.store(vt, tid, all ? nullptr : keep);
+        }
+        __syncthreads();
+    };
     if (t0 < t1) load(t0);
     for (int t = t0; t < t1; ++t) {
-        char *kt = lds + (S::BUFFERS == 2 ? (t & 1) * 2 * S::TILE : 0), *vt = kt + S::TILE;
+        char *kt = buffer(t), *vt = kt + S::TILE;
         uint64_t keep[S::WORDS];
         bool all = true;
 #pragma unroll
@@ -440,27 +545,27 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
             keep[i] = __ballot(seen[i] != 0);
             all &= S::BK - 64 * i >= 64 ? keep[i] == ~0ull : (uint32_t)keep[i] == ~0u;
         }
-        if (S::BUFFERS == 1) __syncthreads();
-        ks.store(kt, tid, nullptr);
-        if (all) vs.store(vt, tid, nullptr);
-        else vs.store(vt, tid, keep);                   // a value that is not seen may be anything: 0 * NaN
-        __syncthreads();
+        arrive(t, keep, all, false);
         if (t + 1 < t1) load(t + 1);
 
+        const int sub = QW == 1 ? kw : 0;               // the first of this wavefront's runs of 32 keys
         f32x16 s[S::NT];
-        float top = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < S::NT; ++i) {
-            const int sub = QW == 1 ? kw : i;
-            s[i] = product<E, D>(kt + 32 * sub * L::STRIDE, S::PLANE, own, lane, f32x16{});
-            if (!all) {
-                const uint32_t bits = (uint32_t)(keep[sub >> 1] >> (32 * (sub & 1))) >> (4 * h);
+        for (int i = 0; i < S::NT; ++i) s[i] = f32x16{};
+        products<E, D, S::NT>(kt + 32 * sub * L::STRIDE, S::PLANE, own, lane, s);
+        Fold<E, D, S::DT> fold(vt + 32 * sub * L::STRIDE, S::PLANE, left);
+        if (!all)
+#pragma unroll
+            for (int i = 0; i < S::NT; ++i) {
+                const uint32_t bits = (uint32_t)(keep[(sub + i) >> 1] >> (32 * ((sub + i) & 1))) >> (4 * h);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) if (!(bits >> reg_row(r) & 1)) s[i][r] = -INFINITY;
             }
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < S::NT; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[i][r]);
-        }
         top = fmaxf(top, other_half(top)) * a.c;
         // The sums are kept relative to a maximum that is brought up only when a score exceeds it by 2^8: exact in
         // fp32 either way (exponents have room), and nearly every tile is spared the scaling of the sums.
@@ -476,14 +581,13 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
         }
         const float base = m == -INFINITY ? 0.f : m;    // no key yet: exp2(-inf) = 0, not -inf + inf
 #pragma unroll
-        for (int i = 0; i < S::NT; ++i) {
+        for (int i = 0; i < S::NT; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[i][r] = exp2_fast(__builtin_fmaf(s[i][r], a.c, -base));
                 l += s[i][r];
             }
-            fold<E, D>(vt + 32 * (QW == 1 ? kw : i) * L::STRIDE, S::PLANE, s[i], left, acc);
-        }
+        fold.run(s, acc);
     }
     l += other_half(l);
 
@@ -524,7 +628,7 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_fwd_kernel(Arg
     const int64_t at = token * a.hq + head;
     const int e0 = 32 * S::DT * dw;
     if (a.splits == 1) {
-        store_row<T>((T *)a.Ow + token * a.ld_o + (int64_t)head * a.d + e0, acc, l > 0.f || l != l ? 1.f / l : 0.f, a.d - e0, a.vec, h);
+        store_row<T>((T *)a.Ow + token * a.ld_o + (int64_t)head * a.d + e0, acc, l > 0.f || l != l ? 1.f / l : 0.f, a.d - e0, VEC, h);
         if (a.lse && h == 0 && dw == 0) a.lse[at] = l > 0.f || l != l ? m * LN2 + logf(l) : -INFINITY;
     } else {
         const int64_t p = (int64_t)split * a.nq * a.hq + at;
@@ -632,10 +736,10 @@ template <int DT, int WAVES> __device__ __forceinline__ void join_waves(char *ld
 }
 
 // dQ, and D for the pass over the keys: the walk of the forward kernel.
-template <typename E, int D, int QW>
-__global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(Args a)
+template <typename E, int D, int QW, bool VEC>
+__global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::DIRECT ? 2 : 1)) void attn_bwd_dq_kernel(Args a)
 {
-    typedef Keys<E, D, QW> S;
+    typedef Keys<E, D, QW, VEC> S;
     typedef Tile<E, D> L;
     typedef typename E::T T;
     __shared__ __align__(16) char lds[S::LDS];
@@ -659,10 +763,10 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(
     const bool part = valid && lse != -INFINITY;        // a row that saw no key: its gradient is zero, whatever dO holds
     const float lse2 = part ? lse * LOG2E : INFINITY;
     Own<E, D> own, grad;
-    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, part, a.d, a.vec, h);
-    grad.load((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d, part, a.d, a.vec, h);
+    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, part, a.d, VEC, h);
+    grad.load((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d, part, a.d, VEC, h);
     const float delta = row_dot<T, D>((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d,
-                                      (const T *)a.O + token * a.ld_o + (int64_t)head * a.d, part, a.d, a.vec, h);
+                                      (const T *)a.O + token * a.ld_o + (int64_t)head * a.d, part, a.d, VEC, h);
     if (valid && split == 0 && kw == 0 && dw == 0 && h == 0) a.delta[at] = delta;
 
     const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
@@ -675,17 +779,42 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(
     f32x16 acc[S::DT];
 #pragma unroll
     for (int dt = 0; dt < S::DT; ++dt) acc[dt] = f32x16{};
-    Stage<E, D, S::BK, S::THREADS> ks, vs;
+    // The next tile is on its way while this one is multiplied: in registers, or straight to the other buffer.
+    typedef Stage<E, D, S::BK, S::THREADS> Regs;
+    typedef Direct<D, S::BK> Dir;
+    Regs ks, vs;
     int seen[S::WORDS];
+    auto buffer = [&](int t) { return lds + (S::BUFFERS == 2 ? (t & 1) * 2 * S::TILE : 0); };
     auto load = [&](int t) {
-        ks.load(kp, a.ld_k, t * S::BK, len, a.d, a.vec, tid);
-        vs.load(vp, a.ld_v, t * S::BK, len, a.d, a.vec, tid);
+        if constexpr (S::DIRECT) {
+            Dir::load(kp, a.ld_k, t * S::BK, len, a.d, buffer(t), wave, lane);
+            Dir::load(vp, a.ld_v, t * S::BK, len, a.d, buffer(t) + S::TILE, wave, lane);
+        } else {
+            ks.load(kp, a.ld_k, t * S::BK, len, a.d, VEC, tid);
+            vs.load(vp, a.ld_v, t * S::BK, len, a.d, VEC, tid);
+        }
 #pragma unroll
         for (int i = 0; i < S::WORDS; ++i) seen[i] = key_byte(mask, t * S::BK + 64 * i + lane, len);
     };
+    // tile t in LDS; keys that are not seen as zeros in the second matrix (0 * NaN), and where asked for in the first
+    auto arrive = [&](int t, const uint64_t *keep, bool all, bool both) {
+        char *kt = buffer(t), *vt = kt + S::TILE;
+        if constexpr (S::DIRECT) {
+            Dir::wait();
+            if (!all) {
+                Dir::clear(vt, wave, lane, keep[0]);
+                if (both) Dir::clear(kt, wave, lane, keep[0]);
+            }
+        } else {
+            if (S::BUFFERS == 1) __syncthreads();
+            ks.store(kt, tid, all || !both ? nullptr : keep);
+            vs.store(vt, tid, all ? nullptr : keep);
+        }
+        __syncthreads();
+    };
     if (t0 < t1) load(t0);
     for (int t = t0; t < t1; ++t) {
-        char *kt = lds + (S::BUFFERS == 2 ? (t & 1) * 2 * S::TILE : 0), *vt = kt + S::TILE;
+        char *kt = buffer(t), *vt = kt + S::TILE;
         uint64_t keep[S::WORDS];
         bool all = true;
 #pragma unroll
@@ -693,27 +822,25 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(
             keep[i] = __ballot(seen[i] != 0);
             all &= S::BK - 64 * i >= 64 ? keep[i] == ~0ull : (uint32_t)keep[i] == ~0u;
         }
-        if (S::BUFFERS == 1) __syncthreads();
-        if (all) { ks.store(kt, tid, nullptr); vs.store(vt, tid, nullptr); }
-        else { ks.store(kt, tid, keep); vs.store(vt, tid, keep); }
-        __syncthreads();
+        arrive(t, keep, all, true);
         if (t + 1 < t1) load(t + 1);
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) {
             const int sub = QW == 1 ? kw : i;
-            f32x16 s = product<E, D>(kt + 32 * sub * L::STRIDE, S::PLANE, own, lane, f32x16{});
-            f32x16 g;
+            f32x16 s[1] = {f32x16{}}, g[1];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) g[r] = -delta;
-            g = product<E, D>(vt + 32 * sub * L::STRIDE, S::PLANE, grad, lane, g);
+            for (int r = 0; r < 16; ++r) g[0][r] = -delta;
+            products<E, D, 1>(kt + 32 * sub * L::STRIDE, S::PLANE, own, lane, s);
+            products<E, D, 1>(vt + 32 * sub * L::STRIDE, S::PLANE, grad, lane, g);
+            Fold<E, D, S::DT> fold(kt + 32 * sub * L::STRIDE, S::PLANE, left);
             if (!all) {
                 const uint32_t bits = (uint32_t)(keep[sub >> 1] >> (32 * (sub & 1))) >> (4 * h);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) if (!(bits >> reg_row(r) & 1)) s[r] = -INFINITY;
+                for (int r = 0; r < 16; ++r) if (!(bits >> reg_row(r) & 1)) s[0][r] = -INFINITY;
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) g[r] *= exp2_fast(__builtin_fmaf(s[r], a.c, -lse2));
-            fold<E, D>(kt + 32 * sub * L::STRIDE, S::PLANE, g, left, acc);
+            for (int r = 0; r < 16; ++r) g[0][r] *= exp2_fast(__builtin_fmaf(s[0][r], a.c, -lse2));
+            fold.run(g, acc);
         }
     }
     if constexpr (QW == 1) {
@@ -722,7 +849,7 @@ __global__ __launch_bounds__((Keys<E, D, QW>::THREADS)) void attn_bwd_dq_kernel(
     }
     if (!valid) return;
     const int e0 = 32 * S::DT * dw;
-    if (a.splits == 1) store_row<T>((T *)a.dQ + token * a.ld_dq + (int64_t)head * a.d + e0, acc, a.scale, a.d - e0, a.vec, h);
+    if (a.splits == 1) store_row<T>((T *)a.dQ + token * a.ld_dq + (int64_t)head * a.d + e0, acc, a.scale, a.d - e0, VEC, h);
     else store_row<float>(a.part + ((int64_t)split * a.nq * a.hq + at) * a.d + e0, acc, a.scale, a.d - e0, a.d % 4 == 0, h);
 }
 
@@ -740,18 +867,19 @@ template <typename T> __global__ __launch_bounds__(256) void attn_bwd_join_kerne
 // dK and dV: a wavefront has 32 keys, the queries of all heads that share their head stream past, one head after
 // the other, so the sum over them is taken in registers in a fixed order.  KW wavefronts have keys of their own (4, wide)
 // or all share 32 keys and deal the queries of a tile among them (1, narrow).
-template <typename E, int D, int KW> struct Queries {
+template <typename E, int D, int KW, bool VEC> struct Queries {
     static constexpr int WAVES = 4, THREADS = 64 * WAVES, DW = KW == 1 && E::PLANES == 3 && D > 64 ? 2 : 1, QW = WAVES / KW / DW, BK = 32 * KW;
     static constexpr int DT = D / 32 / DW;
     static constexpr int BR = KW == 1 ? 32 * QW : E::PLANES == 1 ? 64 : 32, NT = BR / 32 / QW;
     static constexpr int PLANE = BR * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE, BUFFER = 2 * TILE + 2 * BR * 4;
     static constexpr int BUFFERS = KW == 1 || 2 * BUFFER > 80 * 1024 ? 1 : 2;
+    static constexpr bool DIRECT = VEC && E::PLANES == 1 && KW == 4;
     static constexpr int JOIN = KW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = BUFFERS * BUFFER > JOIN ? BUFFERS * BUFFER : JOIN;
 };
-template <typename E, int D, int KW>
-__global__ __launch_bounds__((Queries<E, D, KW>::THREADS)) void attn_bwd_dkv_kernel(Args a)
+template <typename E, int D, int KW, bool VEC>
+__global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, KW, VEC>::DIRECT && D < 128 ? 2 : 1)) void attn_bwd_dkv_kernel(Args a)
 {
-    typedef Queries<E, D, KW> S;
+    typedef Queries<E, D, KW, VEC> S;
     typedef Tile<E, D> L;
     typedef typename E::T T;
     __shared__ __align__(16) char lds[S::LDS];
@@ -768,8 +896,8 @@ __global__ __launch_bounds__((Queries<E, D, KW>::THREADS)) void attn_bwd_dkv_ker
     const int64_t key = k.begin + (int64_t)tile * S::BK + 32 * kw + (lane & 31);
     const bool valid = key < k.end, seen = valid && (!a.mask || a.mask[key]);
     Own<E, D> kk, vv;
-    kk.load((const T *)a.K + (valid ? key : 0) * a.ld_k + (int64_t)kvh * a.d, seen, a.d, a.vec, h);
-    vv.load((const T *)a.V + (valid ? key : 0) * a.ld_v + (int64_t)kvh * a.d, seen, a.d, a.vec, h);
+    kk.load((const T *)a.K + (valid ? key : 0) * a.ld_k + (int64_t)kvh * a.d, seen, a.d, VEC, h);
+    vv.load((const T *)a.V + (valid ? key : 0) * a.ld_v + (int64_t)kvh * a.d, seen, a.d, VEC, h);
 
     const int len = q.end - q.begin, tiles = (len + S::BR - 1) / S::BR, steps = tiles * a.group;
     const int left = Layout<D>::left(Layout<D>::left0(lane), S::DT * dw);
@@ -777,11 +905,20 @@ __global__ __launch_bounds__((Queries<E, D, KW>::THREADS)) void attn_bwd_dkv_ker
 #pragma unroll
     for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
 
-    Stage<E, D, S::BR, S::THREADS> qs, gs;
+    typedef Stage<E, D, S::BR, S::THREADS> Regs;
+    typedef Direct<D, S::BR> Dir;
+    Regs qs, gs;
     float lse = 0.f, delta = 0.f;
-    auto load = [&](int head, int t) {
-        qs.load((const T *)a.Q + q.begin * a.ld_q + (int64_t)head * a.d, a.ld_q, t * S::BR, len, a.d, a.vec, tid);
-        gs.load((const T *)a.dO + q.begin * a.ld_do + (int64_t)head * a.d, a.ld_do, t * S::BR, len, a.d, a.vec, tid);
+    auto buffer = [&](int step) { return lds + (S::BUFFERS == 2 ? (step & 1) * S::BUFFER : 0); };
+    auto load = [&](int step, int head, int t) {
+        const T *qp = (const T *)a.Q + q.begin * a.ld_q + (int64_t)head * a.d, *gp = (const T *)a.dO + q.begin * a.ld_do + (int64_t)head * a.d;
+        if constexpr (S::DIRECT) {
+            Dir::load(qp, a.ld_q, t * S::BR, len, a.d, buffer(step), wave, lane);
+            Dir::load(gp, a.ld_do, t * S::BR, len, a.d, buffer(step) + S::TILE, wave, lane);
+        } else {
+            qs.load(qp, a.ld_q, t * S::BR, len, a.d, VEC, tid);
+            gs.load(gp, a.ld_do, t * S::BR, len, a.d, VEC, tid);
+        }
         if (tid < S::BR) {
             const int row = t * S::BR + tid;
             const int64_t at = (int64_t)(q.begin + row) * a.hq + head;
@@ -790,40 +927,48 @@ __global__ __launch_bounds__((Queries<E, D, KW>::THREADS)) void attn_bwd_dkv_ker
         }
     };
     int head = kvh * a.group, t = 0;
-    if (steps) load(head, 0);
+    if (steps) load(0, head, 0);
     for (int step = 0; step < steps; ++step) {
-        char *qt = lds + (S::BUFFERS == 2 ? (step & 1) * S::BUFFER : 0), *gt = qt + S::TILE;
+        char *qt = buffer(step), *gt = qt + S::TILE;
         float *stat = (float *)(gt + S::TILE);
-        if (S::BUFFERS == 1) __syncthreads();
-        qs.store(qt, tid, nullptr);
-        gs.store(gt, tid, nullptr);
+        if constexpr (S::DIRECT) {
+            Dir::wait();
+        } else {
+            if (S::BUFFERS == 1) __syncthreads();
+            qs.store(qt, tid, nullptr);
+            gs.store(gt, tid, nullptr);
+        }
         if (tid < S::BR) {
             stat[tid] = lse == -INFINITY ? -INFINITY : -lse * LOG2E;    // no such row, or one that saw no key: p = 0
             stat[S::BR + tid] = -delta;
         }
         __syncthreads();
         if (++t == tiles) { t = 0; ++head; }
-        if (step + 1 < steps) load(head, t);
+        if (step + 1 < steps) load(step + 1, head, t);
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) {
             const int sub = KW == 1 ? qw : i;
-            f32x16 p = product<E, D>(qt + 32 * sub * L::STRIDE, S::PLANE, kk, lane, f32x16{});
-            f32x16 g;
+            f32x16 p[1] = {f32x16{}}, g[1];
+            f32x4 x[4];
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const f32x4 x = *(const f32x4 *)(stat + 32 * sub + reg_row(r) + 4 * h);
-                const f32x4 y = *(const f32x4 *)(stat + S::BR + 32 * sub + reg_row(r) + 4 * h);
+            for (int r = 0; r < 4; ++r) {
+                x[r] = *(const f32x4 *)(stat + 32 * sub + 8 * r + 4 * h);
+                const f32x4 y = *(const f32x4 *)(stat + S::BR + 32 * sub + 8 * r + 4 * h);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    p[r + j] = exp2_fast(__builtin_fmaf(p[r + j], a.c, x[j]));
-                    g[r + j] = y[j];
-                }
+                for (int j = 0; j < 4; ++j) g[0][4 * r + j] = y[j];
             }
-            g = product<E, D>(gt + 32 * sub * L::STRIDE, S::PLANE, vv, lane, g);
-            fold<E, D>(gt + 32 * sub * L::STRIDE, S::PLANE, p, left, dv);
+            products<E, D, 1>(qt + 32 * sub * L::STRIDE, S::PLANE, kk, lane, p);
+            products<E, D, 1>(gt + 32 * sub * L::STRIDE, S::PLANE, vv, lane, g);
+            {
+                Fold<E, D, S::DT> fold(gt + 32 * sub * L::STRIDE, S::PLANE, left);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) g[r] *= p[r];
-            fold<E, D>(qt + 32 * sub * L::STRIDE, S::PLANE, g, left, dk);
+                for (int r = 0; r < 16; ++r) p[0][r] = exp2_fast(__builtin_fmaf(p[0][r], a.c, x[r >> 2][r & 3]));
+                fold.run(p, dv);
+            }
+            Fold<E, D, S::DT> fold(qt + 32 * sub * L::STRIDE, S::PLANE, left);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[0][r] *= p[0][r];
+            fold.run(g, dk);
         }
     }
     if constexpr (KW == 1) {
@@ -836,8 +981,8 @@ __global__ __launch_bounds__((Queries<E, D, KW>::THREADS)) void attn_bwd_dkv_ker
 #pragma unroll
         for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
     const int e0 = 32 * S::DT * dw;
-    store_row<T>((T *)a.dK + key * a.ld_dk + (int64_t)kvh * a.d + e0, dk, a.scale, a.d - e0, a.vec, h);
-    store_row<T>((T *)a.dV + key * a.ld_dv + (int64_t)kvh * a.d + e0, dv, 1.f, a.d - e0, a.vec, h);
+    store_row<T>((T *)a.dK + key * a.ld_dk + (int64_t)kvh * a.d + e0, dk, a.scale, a.d - e0, VEC, h);
+    store_row<T>((T *)a.dV + key * a.ld_dv + (int64_t)kvh * a.d + e0, dv, 1.f, a.d - e0, VEC, h);
 }
 
 }  // namespace attn

@@ -17,12 +17,16 @@ template <typename T> struct EngineOf { typedef Bf16 E; };
 template <> struct EngineOf<float> { typedef Split E; };
 
 // The instance for heads of d channels.  fp32's narrow forms share a result's channels between two wavefronts beyond 64: no 96.
-template <typename T, typename F> void with_width(int d, bool narrow, F &&f)
+template <typename T, typename F> void with_width(int d, bool narrow, bool vec, F &&f)
 {
-    if (d <= 32) f(std::integral_constant<int, 32>{});
-    else if (d <= 64) f(std::integral_constant<int, 64>{});
-    else if (d <= 96 && !(narrow && sizeof(T) == 4)) f(std::integral_constant<int, 96>{});
-    else f(std::integral_constant<int, 128>{});
+    auto g = [&](auto w) {
+        if (vec) f(w, std::true_type{});
+        else f(w, std::false_type{});
+    };
+    if (d <= 32) g(std::integral_constant<int, 32>{});
+    else if (d <= 64) g(std::integral_constant<int, 64>{});
+    else if (d <= 96 && !(narrow && sizeof(T) == 4)) g(std::integral_constant<int, 96>{});
+    else g(std::integral_constant<int, 128>{});
 }
 template <typename T, int D> constexpr bool has_narrow = sizeof(T) == 2 || D != 96;
 
@@ -30,15 +34,16 @@ template <typename T> hch_status launch_fwd(const Args &a, bool narrow, double b
 {
     {
         LaunchTimer lt(HCH_KERNEL_ID("attn_fwd_kernel"), s, bytes, flops);
-        with_width<T>(a.d, narrow, [&](auto w) {
+        with_width<T>(a.d, narrow, a.vec, [&](auto w, auto v) {
             typedef typename EngineOf<T>::E E;
             constexpr int D = decltype(w)::value;
+            constexpr bool V = decltype(v)::value;
             if (!narrow) {
-                constexpr auto kernel = attn_fwd_kernel<E, D, 4>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 4>::THREADS)), 0, s, a);
+                constexpr auto kernel = attn_fwd_kernel<E, D, 4, V>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
             } else if constexpr (has_narrow<T, D>) {
-                constexpr auto kernel = attn_fwd_kernel<E, D, 1>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 1>::THREADS)), 0, s, a);
+                constexpr auto kernel = attn_fwd_kernel<E, D, 1, V>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
             }
         });
     }
@@ -61,15 +66,16 @@ template <typename T> hch_status launch_bwd_dq(const Args &a, bool narrow, doubl
 {
     {
         LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_dq_kernel"), s, bytes, flops);
-        with_width<T>(a.d, narrow, [&](auto w) {
+        with_width<T>(a.d, narrow, a.vec, [&](auto w, auto v) {
             typedef typename EngineOf<T>::E E;
             constexpr int D = decltype(w)::value;
+            constexpr bool V = decltype(v)::value;
             if (!narrow) {
-                constexpr auto kernel = attn_bwd_dq_kernel<E, D, 4>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 4>::THREADS)), 0, s, a);
+                constexpr auto kernel = attn_bwd_dq_kernel<E, D, 4, V>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
             } else if constexpr (has_narrow<T, D>) {
-                constexpr auto kernel = attn_bwd_dq_kernel<E, D, 1>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 1>::THREADS)), 0, s, a);
+                constexpr auto kernel = attn_bwd_dq_kernel<E, D, 1, V>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
             }
         });
     }
@@ -89,15 +95,16 @@ template <typename T> hch_status launch_bwd_dkv(const Args &a, bool narrow, doub
 {
     {
         LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_dkv_kernel"), s, bytes, flops);
-        with_width<T>(a.d, narrow, [&](auto w) {
+        with_width<T>(a.d, narrow, a.vec, [&](auto w, auto v) {
             typedef typename EngineOf<T>::E E;
             constexpr int D = decltype(w)::value;
+            constexpr bool V = decltype(v)::value;
             if (!narrow) {
-                constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 4>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Queries<E, D, 4>::THREADS)), 0, s, a);
+                constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 4, V>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Queries<E, D, 4, V>::THREADS)), 0, s, a);
             } else if constexpr (has_narrow<T, D>) {
-                constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 1>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Queries<E, D, 1>::THREADS)), 0, s, a);
+                constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 1, V>;
+                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Queries<E, D, 1, V>::THREADS)), 0, s, a);
             }
         });
     }
