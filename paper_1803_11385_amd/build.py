@@ -11,10 +11,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhch.so")
 SOURCES = ["hch_api.hip", "psh_build.cpp", "norm_rope.hip", "attn_bf16.hip", "attn_f32.hip", "attn_api.hip"]
-# hch_api.hip, attn_bf16.hip: accumulators of the matrix instructions in ordinary VGPRs, updated in place: with
+# accumulators of the matrix instructions in ordinary VGPRs, updated in place: with
 # the default (AGPR) form the compiler copies every accumulator through VGPRs once per loop
 # iteration, which costs the bf16 kernels more issue slots than their matrix instructions
-VGPR_FORM = ("hch_api.hip", "attn_bf16.hip")
+VGPR_FORM = ("hch_api.hip", "attn_bf16.hip", "attn_f32.hip")
 HEADERS = ["kernels.hip.hpp", "direct.hip.hpp", "gemm_bf16.hip.hpp", "split_wgrad.hip.hpp", "split_conv.hip.hpp", "conv_small.hip.hpp", "split_columns.hip.hpp", "split_dcol.hip.hpp", "split_field.hip.hpp", "conv_bf16.hip.hpp", "psh_device.hip.hpp", "occupancy.hip.hpp", "psh_build.hpp", "profile.hpp", "api_common.hpp", "norm.hip.hpp", "rope.hip.hpp", "attn.hip.hpp", "attn_launch.hpp", os.path.join("..", "..", "include", "hch.h")]
 
 

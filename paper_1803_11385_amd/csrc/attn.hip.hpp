@@ -392,16 +392,20 @@ __device__ __forceinline__ void products(const char *tile, int plane, const Own<
     }
 }
 
-// acc[dt] += (rows of a tile, transposed) p, for the channels from `left`'s on, 16 rows at a time.  The first 16 rows' operands
-// are read by the constructor, so that they arrive while p is still being made.
+// acc[dt] += (rows of a tile, transposed) p, for the channels from `left`'s on, 16 rows at a time.  The first operands are read
+// by the constructor, so that they arrive while p is still being made.
 template <typename E, int D, int DT> struct Fold {
-    typename E::Part a[2][DT];
+    static constexpr int G = E::PLANES == 1 ? DT : 1;       // operands read ahead
+    typename E::Part a[2][G];
     const char *tile;
     int plane, left;
-    __device__ __forceinline__ void read(int step)
+    __device__ __forceinline__ void read(int g)
     {
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) a[step & 1][dt] = E::template cols<D>(tile + 16 * step * Tile<E, D>::STRIDE, plane, Layout<D>::left(left, dt));
+        for (int i = 0; i < G; ++i) {
+            const int step = (g * G + i) / DT, dt = (g * G + i) % DT;
+            a[g & 1][i] = E::template cols<D>(tile + 16 * step * Tile<E, D>::STRIDE, plane, Layout<D>::left(left, dt));
+        }
     }
     __device__ __forceinline__ Fold(const char *t, int pl, int l) : tile(t), plane(pl), left(l)
     {
@@ -410,13 +414,14 @@ template <typename E, int D, int DT> struct Fold {
     }
     template <int N> __device__ __forceinline__ void run(const f32x16 (&p)[N], f32x16 (&acc)[DT])
     {
+        typename E::Part b;
 #pragma unroll
-        for (int step = 0; step < 2 * N; ++step) {
-            if (step + 1 < 2 * N) read(step + 1);
+        for (int g = 0; g * G < 2 * N * DT; ++g) {
+            if ((g + 1) * G < 2 * N * DT) read(g + 1);
             keep_order();
-            const typename E::Part b = E::col(p[step >> 1], step & 1);
+            if (g * G % DT == 0) b = E::col(p[g * G / DT >> 1], g * G / DT & 1);
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) acc[dt] = E::mul(a[step & 1][dt], b, acc[dt]);
+            for (int i = 0; i < G; ++i) acc[(g * G + i) % DT] = E::mul(a[g & 1][i], b, acc[(g * G + i) % DT]);
             keep_order();
         }
     }
