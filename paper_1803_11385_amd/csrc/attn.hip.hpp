@@ -46,7 +46,7 @@ struct Args {
     float *delta;                          // [n_q * hq] D
     int64_t nq, nk, ld_q, ld_k, ld_v, ld_o, ld_do, ld_dq, ld_dk, ld_dv;
     int batch, hq, hkv, group, d;
-    int slots, splits, total;              // tiles per head at most, splits over the streamed rows, slots * heads * splits
+    int slots, splits, run, per_head;      // tiles per head at most, splits over the streamed rows; see work_item
     int vec;                               // everything in 16-byte pieces
     float scale, c;                        // c = scale log2(e)
 };
@@ -198,11 +198,25 @@ __device__ __forceinline__ constexpr int reg_row(int r) { return 8 * (r >> 2) + 
 // ---------------------------------------------------------------------------------------------
 // work distribution
 // ---------------------------------------------------------------------------------------------
-// Workgroups go to the 8 XCDs in turn; runs of RUN neighbours in the work list are kept on one, so that the tiles that
-// read the same keys share its L2, while shapes of different lengths still spread over all of them.
-constexpr int RUN = 16;
-__device__ __forceinline__ int work_item(int id) { return ((id >> 3) / RUN * 8 + (id & 7)) * RUN + (id >> 3) % RUN; }
-inline unsigned work_grid(int total) { return (unsigned)((total + 8 * RUN - 1) / (8 * RUN) * (8 * RUN)); }
+// Workgroups go to the 8 XCDs in turn; runs of `run` neighbours in the work list are kept on one, so that the tiles that
+// read the same keys share its L2, while shapes of different lengths still spread over all of them.  Runs are short where there
+// are few workgroups, or some XCDs would get more than others: 512 of dQ (8 shapes of 2000 rows, 32 channels, fp32) took 108 us
+// in runs of 16 and take 81 one by one.
+// A head's part of the list is a whole number of turns, so that heads that share lines of memory meet on one XCD.
+__device__ __forceinline__ int work_item(int id, int run) { return ((id >> 3) / run * 8 + (id & 7)) * run + (id >> 3) % run; }
+inline void set_work(Args &a)
+{
+    const int64_t each = (int64_t)a.slots * a.splits, total = each * a.hkv;
+    a.run = total >= 4096 ? 16 : total >= 1024 ? 4 : 1;
+    a.per_head = (int)((each + 8 * a.run - 1) / (8 * a.run) * (8 * a.run));
+}
+inline unsigned work_grid(const Args &a) { return (unsigned)a.per_head * (unsigned)a.hkv; }
+struct Work { int head, slot, split; };         // slot beyond the last: nothing to do
+__device__ __forceinline__ Work work_of(const Args &a, int id)
+{
+    const int w = work_item(id, a.run), head = w / a.per_head, rest = w - head * a.per_head, slot = rest / a.splits;
+    return {head, slot, rest - slot * a.splits};
+}
 
 // A shape's rows [begin, end) of n, safe whatever the offsets hold.
 struct Span { int begin, end; };
@@ -479,9 +493,9 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave % S::KW : 0, dw = QW == 1 ? wave / S::KW : 0;
-    const int w = work_item(blockIdx.x);
-    if (w >= a.total) return;
-    const int split = w % a.splits, slot = w / a.splits % a.slots, kvh = w / a.splits / a.slots;
+    const Work w = work_of(a, blockIdx.x);
+    const int split = w.split, slot = w.slot, kvh = w.head;
+    if (slot >= a.slots) return;
     const int b = shape_of_slot(a.qo, a.batch, a.nq, a.group, S::BQ, slot, lane);
     const Span q = span_of(a.qo, b, a.nq), k = span_of(a.ko, b, a.nk);
     const int tile = slot - first_slot(q.begin, a.group, S::BQ, b);
@@ -643,31 +657,60 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
 }
 
 // Joins the splits of a row: G groups of 32 lanes deal the splits among them, a lane has 4 channels.  8 groups for a row
-// where there are few rows of many splits; else a group for each (10778 rows x 2 heads of 3 splits: 34 -> 5 us).
+// where there are few rows of many splits; else a group for each (10778 rows x 2 heads of 3 splits: 34 -> 5 us).  A group
+// first turns its splits' maxima into weights, 32 at a time, then adds their sums up without waiting for one before the next
+// (64 rows of 128 splits: 16 -> 6 us).
 template <typename T, int G> __global__ __launch_bounds__(256) void attn_join_kernel(Args a)
 {
     __shared__ __align__(16) float sums[8][128];
+    __shared__ float weight[8][32];
     __shared__ float2 ml[8];
     const int x = threadIdx.x & 31, group = threadIdx.x >> 5, g = group % G;
     const int64_t rows = a.nq * a.hq, at = (int64_t)blockIdx.x * (8 / G) + group / G;
     const bool there = at < rows, whole = a.d % 4 == 0;
     float m = -INFINITY, l = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (there) {
-        for (int s = g; s < a.splits; s += G) m = fmaxf(m, a.ml[s * rows + at].x);
-        for (int s = g; s < a.splits; s += G) {
-            const float2 v = a.ml[s * rows + at];
-            if (!(v.y > 0.f || v.y != v.y)) continue;   // a split without a key has written no sums
-            const float f = exp2_fast(v.x - m);
-            l += f * v.y;
-            const float *p = a.part + (s * rows + at) * a.d + 4 * x;
-            if (4 * x < a.d) {
-                if (whole) acc += f * *(const f32x4 *)p;
-                else
+    const int mine = there ? (a.splits - g + G - 1) / G : 0;        // splits g, g + G, ...
+    for (int first = 0; first < mine; first += 32) {
+        const int n = min(32, mine - first);
+        float2 v = make_float2(-INFINITY, 0.f);
+        if (x < n) v = a.ml[(int64_t)(g + G * (first + x)) * rows + at];
+        const bool some = v.y > 0.f || v.y != v.y;      // a split without a key has written no sums
+        float top = m;
+        {
+            float t = some ? v.x : -INFINITY;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) if (4 * x + j < a.d) acc[j] += f * p[j];
-            }
+            for (int i = 16; i; i >>= 1) t = fmaxf(t, __shfl_xor(t, i));
+            top = fmaxf(m, t);
         }
+        const float w = some ? exp2_fast(v.x - top) : 0.f, old = m == -INFINITY ? 0.f : exp2_fast(m - top);
+        float sum = some ? w * v.y : 0.f;
+#pragma unroll
+        for (int i = 16; i; i >>= 1) sum += __shfl_xor(sum, i);
+        l = l * old + sum;
+        acc *= old;
+        m = top;
+        weight[group][x] = w;
+        __builtin_amdgcn_wave_barrier();
+        const float *p = a.part + ((int64_t)(g + G * first) * rows + at) * a.d + 4 * x;
+        const int64_t step = (int64_t)G * rows * a.d;
+        if (4 * x < a.d) {
+            if (whole) {
+#pragma unroll 8
+                for (int i = 0; i < n; ++i) {
+                    const f32x4 t = *(const f32x4 *)(p + i * step);
+                    const float f = weight[group][i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[j] += f == 0.f ? 0.f : f * t[j];
+                }
+            } else
+                for (int i = 0; i < n; ++i) {
+                    const float f = weight[group][i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) if (4 * x + j < a.d) acc[j] += f == 0.f ? 0.f : f * p[i * step + j];
+                }
+        }
+        __builtin_amdgcn_wave_barrier();
     }
     if constexpr (G > 1) {
         *(f32x4 *)&sums[g][4 * x] = acc;
@@ -750,9 +793,9 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave % S::KW : 0, dw = QW == 1 ? wave / S::KW : 0;
-    const int w = work_item(blockIdx.x);
-    if (w >= a.total) return;
-    const int split = w % a.splits, slot = w / a.splits % a.slots, kvh = w / a.splits / a.slots;
+    const Work w = work_of(a, blockIdx.x);
+    const int split = w.split, slot = w.slot, kvh = w.head;
+    if (slot >= a.slots) return;
     const int b = shape_of_slot(a.qo, a.batch, a.nq, a.group, S::BQ, slot, lane);
     const Span q = span_of(a.qo, b, a.nq), k = span_of(a.ko, b, a.nk);
     const int tile = slot - first_slot(q.begin, a.group, S::BQ, b);
@@ -890,9 +933,9 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
     __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int kw = KW == 1 ? 0 : wave, qw = KW == 1 ? wave % S::QW : 0, dw = KW == 1 ? wave / S::QW : 0;
-    const int w = work_item(blockIdx.x);
-    if (w >= a.total) return;
-    const int slot = w % a.slots, kvh = w / a.slots;
+    const Work w = work_of(a, blockIdx.x);
+    const int split = w.split, slot = w.slot, kvh = w.head;
+    if (slot >= a.slots) return;
     const int b = shape_of_slot(a.ko, a.batch, a.nk, 1, S::BK, slot, lane);
     const Span q = span_of(a.qo, b, a.nq), k = span_of(a.ko, b, a.nk);
     const int tile = slot - first_slot(k.begin, 1, S::BK, b);
@@ -904,7 +947,8 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
     kk.load((const T *)a.K + (valid ? key : 0) * a.ld_k + (int64_t)kvh * a.d, seen, a.d, VEC, h);
     vv.load((const T *)a.V + (valid ? key : 0) * a.ld_v + (int64_t)kvh * a.d, seen, a.d, VEC, h);
 
-    const int len = q.end - q.begin, tiles = (len + S::BR - 1) / S::BR, steps = tiles * a.group;
+    const int len = q.end - q.begin, tiles = (len + S::BR - 1) / S::BR;
+    const int s0 = (int)((int64_t)tiles * a.group * split / a.splits), s1 = (int)((int64_t)tiles * a.group * (split + 1) / a.splits);
     const int left = Layout<D>::left(Layout<D>::left0(lane), S::DT * dw);
     f32x16 dk[S::DT], dv[S::DT];
 #pragma unroll
@@ -931,9 +975,9 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
             delta = row < len ? a.delta[at] : 0.f;
         }
     };
-    int head = kvh * a.group, t = 0;
-    if (steps) load(0, head, 0);
-    for (int step = 0; step < steps; ++step) {
+    int head = kvh * a.group + (s0 < s1 ? s0 / tiles : 0), t = s0 < s1 ? s0 % tiles : 0;
+    if (s0 < s1) load(s0, head, t);
+    for (int step = s0; step < s1; ++step) {
         char *qt = buffer(step), *gt = qt + S::TILE;
         float *stat = (float *)(gt + S::TILE);
         if constexpr (S::DIRECT) {
@@ -949,7 +993,7 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
         }
         __syncthreads();
         if (++t == tiles) { t = 0; ++head; }
-        if (step + 1 < steps) load(step + 1, head, t);
+        if (step + 1 < s1) load(step + 1, head, t);
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) {
             const int sub = KW == 1 ? qw : i;
@@ -986,8 +1030,27 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
 #pragma unroll
         for (int dt = 0; dt < S::DT; ++dt) dk[dt] = dv[dt] = f32x16{};
     const int e0 = 32 * S::DT * dw;
-    store_row<T>((T *)a.dK + key * a.ld_dk + (int64_t)kvh * a.d + e0, dk, a.scale, a.d - e0, VEC, h);
-    store_row<T>((T *)a.dV + key * a.ld_dv + (int64_t)kvh * a.d + e0, dv, 1.f, a.d - e0, VEC, h);
+    if (a.splits == 1) {
+        store_row<T>((T *)a.dK + key * a.ld_dk + (int64_t)kvh * a.d + e0, dk, a.scale, a.d - e0, VEC, h);
+        store_row<T>((T *)a.dV + key * a.ld_dv + (int64_t)kvh * a.d + e0, dv, 1.f, a.d - e0, VEC, h);
+    } else {
+        const int64_t rows = a.nk * a.hkv;
+        float *p = a.part + ((int64_t)split * 2 * rows + key * a.hkv + kvh) * a.d + e0;
+        store_row<float>(p, dk, a.scale, a.d - e0, a.d % 4 == 0, h);
+        store_row<float>(p + rows * a.d, dv, 1.f, a.d - e0, a.d % 4 == 0, h);
+    }
+}
+
+// dK and dV = the sums of their splits
+template <typename T> __global__ __launch_bounds__(256) void attn_bwd_join_keys_kernel(Args a)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.nk * a.hkv * a.d;
+    if (i >= 2 * n) return;
+    float t = 0.f;
+    for (int s = 0; s < a.splits; ++s) t += a.part[s * 2 * n + i];
+    const int64_t e = i < n ? i : i - n, at = e / a.d, row = at / a.hkv, col = (at - row * a.hkv) * a.d + (e - at * a.d);
+    if (i < n) ((T *)a.dK)[row * a.ld_dk + col] = (T)t;
+    else ((T *)a.dV)[row * a.ld_dv + col] = (T)t;
 }
 
 }  // namespace attn

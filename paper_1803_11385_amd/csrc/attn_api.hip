@@ -11,56 +11,89 @@ using hch::attn::Args;
 int size_of(hch_dtype t) { return t == HCH_F32 ? 4 : 2; }
 size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 
-// How a pass over the keys is cut.
+// How a pass is cut into workgroups.
 struct Plan {
-    bool narrow;           // one row tile of 32 per workgroup, whose wavefronts share the keys
+    bool narrow;           // tiles of 32 rows (keys) whose wavefronts share what streams past, not of 128
+    int splits;            // parts of what streams past, joined by a second launch
     int64_t slots;
-    int splits;
 };
 
-// Workgroups of tiles of `size` rows there will be about (offsets are known on the device only).
-int64_t tiles_of(int64_t rows, int size, int batch, int heads) { return std::max<int64_t>(batch, (rows + size - 1) / size) * heads; }
+// What a pass takes, as a sum of steps (64 streamed rows in bf16, 32 in fp32; narrow 128, and 64 in fp32 beyond 64 channels):
+// microseconds of a step of a workgroup that has a compute unit to itself, by head width up to 32, 64, 96, 128, and
+// how many workgroups a compute unit takes on before that grows in proportion.  START: before and after the steps; JOIN: the
+// launch that joins splits; dQ and the keys' gradients cost so many times as much as the forward pass.  Fitted to
+// 1020 timings (14 batches of 1 to 32 shapes of 80 to 6000 rows and 3 with 1 or 3 queries a shape, both types, three passes, both
+// forms, 1 to 16 splits; the logarithm is off by 0.15 rms): the choice by it takes 1.02 times as long as the best
+// one in the mean, 1.33 at most; always wide tiles without splits 1.9 and 35 times.
+struct Step { double us, at_once; };
+constexpr Step STEP[2][2][4] = {{{{0.93, 1.59}, {1.62, 1.37}, {2.15, 1.03}, {3.51, 1.21}}, {{1.71, 1.87}, {2.90, 0.99}, {3.28, 0.95}, {4.27, 1.18}}},
+                                {{{0.67, 2.61}, {0.84, 1.69}, {1.06, 1.58}, {2.39, 1.96}}, {{0.69, 2.97}, {0.81, 1.72}, {1.21, 1.24}, {3.75, 2.21}}}};
+constexpr double START = 5.3, JOIN = 5.7, FWD = 1.0, DQ = 1.33, DKV = 1.45, JOIN_SPLIT = 0.03, BYTES_PER_US = 4e6, MEMORY = 5e6, UNITS = 256, UNEVEN = 1.25;
 
-// The narrow forms take a quarter of the time for a tile, but hold as much of LDS (in fp32 beyond 32 channels all
-// that a compute unit lets two workgroups have) for a quarter of the rows.  They are taken where a single round of them
-// takes all tiles: measured at (wide workgroups) bf16 10: 45 -> 22 us, 38: 8.7 -> 7.2, 170: 27 -> 34; fp32 to 32 channels 52: 17 -> 13,
-// 192: 20 -> 22; beyond 400: 43 -> 107.
-bool narrow_fits(const hch_attn_desc &p, int64_t wide_workgroups)
+// rows: of the tiles, over all shapes, `heads` times; stream: rows that one of those tiles sees on average; width: bytes of a
+// row's partial sums; moved: bytes of what streams past, all of it once.  Offsets are known on the device only, so
+// shapes count as equal, the longest as UNEVEN times the mean.
+Plan plan(const hch_attn_desc &p, int64_t rows, int heads, double stream, double cost, double width, double moved)
 {
-    return wide_workgroups <= (p.dtype == HCH_BF16 || p.head_dim <= 32 ? 128 : 64);
+    const int type = p.dtype == HCH_BF16, dc = std::min(3, (p.head_dim - 1) / 32);
+    Plan best = {false, 1, 0};
+    double least = 0.0;
+    for (int narrow = 0; narrow < 2; ++narrow) {
+        const Step &st = STEP[type][narrow][dc];
+        const int size = narrow ? 32 : 128, step = narrow ? (!type && dc >= 2 ? 64 : 128) : type ? 64 : 32;
+        const double wgs = std::max<double>(p.batch, (double)rows / size + 0.5 * p.batch) * heads, steps = std::max(1.0, std::ceil(stream / step));
+        // one to three splits, and as many as make whole rounds of workgroups
+        for (int i = 1; i <= 9; ++i) {
+            const int splits = i <= 3 ? i : (int)std::min(256.0, UNITS * (i - 3) / wgs);
+            if (splits < 1 || splits > steps) continue;
+            const double each = std::ceil(wgs * splits / UNITS), busy = each <= 1.0 ? 1.0 : std::max(1.0, each / st.at_once);
+            double us = (START + std::ceil(UNEVEN * steps / splits) * st.us * cost) * busy;
+            // Memory: at its rate if the compute units share evenly, and not with more than two workgroups each at it (8 shapes
+            // of 76165 keys, 2 heads of 32, bf16: 512 workgroups 26 us, 768 33, 1024 42).
+            us = std::max(us, moved / MEMORY * each * UNITS / (wgs * splits) * (each > 2.0 ? 1.2 : 1.0));
+            if (splits > 1) us += JOIN + JOIN_SPLIT * splits + 2.0 * splits * rows * heads * width / BYTES_PER_US;
+            if (best.slots == 0 || us < least) {
+                least = us;
+                best = {narrow != 0, splits, 1};
+            }
+        }
+    }
+    return best;
 }
 
-Plan plan_keys(const hch_attn_desc &p)
+double row_bytes(const hch_attn_desc &p, int q, int k) { return (double)size_of(p.dtype) * p.head_dim * ((double)q * p.n_q * p.heads_q + (double)k * p.n_k * p.heads_kv); }
+
+Plan plan_keys(const hch_attn_desc &p, double cost)     // forward and dQ: tiles of query rows, keys stream past
 {
     const int group = p.heads_q / p.heads_kv;
-    Plan r;
-    r.narrow = p.n_q * group <= (int64_t)32 * p.batch || narrow_fits(p, tiles_of(p.n_q * group, 128, p.batch, p.heads_kv));
-    const int bq = r.narrow ? 32 : 128;
-    r.slots = hch::attn::slots_of(p.n_q, group, bq, p.batch);
-    // Where the workgroups do not fill the chip (256 compute units with 4 or 2 of them), the keys are split among
-    // several and the parts joined by a second launch.
-    const int64_t wgs = tiles_of(p.n_q * group, bq, p.batch, p.heads_kv);
-    const int64_t tiles = p.n_k / p.batch / (r.narrow ? 128 : 64), want = r.narrow ? 1024 : 512;
-    r.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / std::max<int64_t>(1, wgs), tiles / (r.narrow ? 2 : 4), 256}));
+    Plan r = plan(p, p.n_q * group, p.heads_kv, (double)p.n_k / p.batch, cost, 4.0 * p.head_dim, row_bytes(p, 0, 2));
+    r.slots = hch::attn::slots_of(p.n_q, group, r.narrow ? 32 : 128, p.batch);
     return r;
 }
 
-bool narrow_queries(const hch_attn_desc &p) { return narrow_fits(p, tiles_of(p.n_k, 128, p.batch, p.heads_kv)); }
+Plan plan_queries(const hch_attn_desc &p)               // dK and dV: tiles of keys, the queries of a head's group stream past
+{
+    const int group = p.heads_q / p.heads_kv;
+    Plan r = plan(p, p.n_k, p.heads_kv, (double)p.n_q / p.batch * group, DKV, 8.0 * p.head_dim, row_bytes(p, 2, 0));
+    r.slots = hch::attn::slots_of(p.n_k, 1, r.narrow ? 32 : 128, p.batch);
+    return r;
+}
 
 size_t part_bytes(const hch_attn_desc &p, int splits) { return splits > 1 ? round256((size_t)splits * p.n_q * p.heads_q * p.head_dim * 4) : 0; }
 size_t ml_bytes(const hch_attn_desc &p, int splits) { return splits > 1 ? round256((size_t)splits * p.n_q * p.heads_q * 8) : 0; }
+size_t key_part_bytes(const hch_attn_desc &p, int splits) { return splits > 1 ? round256((size_t)splits * p.n_k * p.heads_kv * p.head_dim * 8) : 0; }
 size_t delta_bytes(const hch_attn_desc &p) { return round256((size_t)p.n_q * p.heads_q * 4); }
 
 size_t fwd_bytes(const hch_attn_desc &p)
 {
     if (!p.batch || !p.n_q) return 256;
-    const Plan r = plan_keys(p);
+    const Plan r = plan_keys(p, FWD);
     return std::max<size_t>(256, part_bytes(p, r.splits) + ml_bytes(p, r.splits));
 }
-size_t bwd_bytes(const hch_attn_desc &p)
+size_t bwd_bytes(const hch_attn_desc &p)            // the parts of dQ are joined before those of dK and dV are written
 {
     if (!p.batch || !p.n_q) return 256;
-    return std::max<size_t>(256, part_bytes(p, plan_keys(p).splits) + delta_bytes(p));
+    return delta_bytes(p) + std::max<size_t>({256, part_bytes(p, plan_keys(p, DQ).splits), key_part_bytes(p, plan_queries(p).splits)});
 }
 
 // what both calls and the size query ask of the sizes
@@ -75,9 +108,11 @@ hch_status check_sizes(const char *who, const hch_attn_desc *p)
     if (p->n_k > 0x7fffffff || p->n_q > 0x7fffffff / p->heads_q) return fail(HCH_EUNSUPPORTED, name + ": more than 2^31 - 1 rows");
     if (p->batch == 0 && (p->n_q || p->n_k)) return fail(HCH_EINVAL, name + ": rows without a shape");
     const int64_t group = p->heads_q / p->heads_kv;
-    if (p->batch && (hch::attn::slots_of(p->n_q, (int)group, 32, p->batch) * p->heads_kv * 2 + 1024 > 0x7fffffff ||
-                     hch::attn::slots_of(p->n_k, 1, 32, p->batch) * p->heads_kv + 1024 > 0x7fffffff))
-        return fail(HCH_EUNSUPPORTED, name + ": too many rows for one launch");
+    if (p->batch) {
+        const Plan a = plan_keys(*p, FWD), b = plan_queries(*p), c = plan_keys(*p, DQ);
+        if (std::max({a.slots * a.splits, b.slots * b.splits, c.slots * c.splits}) > 0x7fffffff / p->heads_kv - 256 || group > 0x7fff)
+            return fail(HCH_EUNSUPPORTED, name + ": too many rows for one launch");
+    }
     return HCH_OK;
 }
 
@@ -118,7 +153,6 @@ bool whole(const hch_attn_desc &p, std::initializer_list<const void *> ptr, std:
 
 // Query-key pairs if the batch were of equal shapes: for the profile's counts, which know no offsets.
 double pairs(const hch_attn_desc &p) { return (double)p.n_q * p.n_k / std::max(1, p.batch) * p.heads_q * p.head_dim; }
-double row_bytes(const hch_attn_desc &p, int q, int k) { return (double)size_of(p.dtype) * p.head_dim * ((double)q * p.n_q * p.heads_q + (double)k * p.n_k * p.heads_kv); }
 
 }  // namespace
 
@@ -139,11 +173,11 @@ extern "C" hch_status hch_attn_fwd(const hch_attn_desc *desc, const void *Q, con
     const hch_attn_desc &p = *desc;
     if ((p.n_q && (!Q || !O)) || (p.n_k && (!K || !V))) return fail(HCH_EINVAL, "hch_attn_fwd: null pointer");
     if (!p.n_q) return HCH_OK;
-    const Plan r = plan_keys(p);
+    const Plan r = plan_keys(p, FWD);
     Args a = args_of(p);
     a.Q = Q; a.K = K; a.V = V; a.Ow = O; a.lse = lse;
     a.vec = whole(p, {Q, K, V, O}, {p.ld_q, p.ld_k, p.ld_v, p.ld_o});
-    a.slots = (int)r.slots; a.splits = r.splits; a.total = a.slots * a.splits * a.hkv;
+    a.slots = (int)r.slots; a.splits = r.splits; hch::attn::set_work(a);
     a.part = (float *)workspace;
     a.ml = (float2 *)((char *)workspace + part_bytes(p, r.splits));
     const double bytes = row_bytes(p, 2, 2), flops = 4 * pairs(p);
@@ -167,8 +201,8 @@ extern "C" hch_status hch_attn_bwd(const hch_attn_desc *desc, const void *Q, con
     a.vec = whole(p, {Q, K, V, O, dO, dQ, dK, dV}, {p.ld_q, p.ld_k, p.ld_v, p.ld_o, p.ld_do, p.ld_dq, p.ld_dk, p.ld_dv});
     const hipStream_t s = (hipStream_t)stream;
     if (p.n_q) {
-        const Plan r = plan_keys(p);
-        a.slots = (int)r.slots; a.splits = r.splits; a.total = a.slots * a.splits * a.hkv;
+        const Plan r = plan_keys(p, DQ);
+        a.slots = (int)r.slots; a.splits = r.splits; hch::attn::set_work(a);
         a.delta = (float *)workspace;
         a.part = (float *)((char *)workspace + delta_bytes(p));
         const double bytes = row_bytes(p, 4, 2), flops = 6 * pairs(p);
@@ -177,11 +211,12 @@ extern "C" hch_status hch_attn_bwd(const hch_attn_desc *desc, const void *Q, con
         if (st != HCH_OK) return st;
     }
     if (p.n_k) {
-        const bool narrow = narrow_queries(p);
-        a.slots = (int)hch::attn::slots_of(p.n_k, 1, narrow ? 32 : 128, p.batch); a.splits = 1; a.total = a.slots * a.hkv;
+        const Plan r = p.n_q ? plan_queries(p) : Plan{false, 1, hch::attn::slots_of(p.n_k, 1, 128, p.batch)};
+        a.slots = (int)r.slots; a.splits = r.splits; hch::attn::set_work(a);
+        a.part = (float *)((char *)workspace + delta_bytes(p));
         const double bytes = row_bytes(p, 2, 4), flops = 8 * pairs(p);
-        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dkv<float>(a, narrow, bytes, flops, s)
-                                : hch::attn::launch_bwd_dkv<__bf16>(a, narrow, bytes, flops, s);
+        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dkv<float>(a, r.narrow, bytes, flops, s)
+                                : hch::attn::launch_bwd_dkv<__bf16>(a, r.narrow, bytes, flops, s);
     }
     return st;
 }

@@ -40,10 +40,10 @@ template <typename T> hch_status launch_fwd(const Args &a, bool narrow, double b
             constexpr bool V = decltype(v)::value;
             if (!narrow) {
                 constexpr auto kernel = attn_fwd_kernel<E, D, 4, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
+                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
             } else if constexpr (has_narrow<T, D>) {
                 constexpr auto kernel = attn_fwd_kernel<E, D, 1, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
+                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
             }
         });
     }
@@ -72,10 +72,10 @@ template <typename T> hch_status launch_bwd_dq(const Args &a, bool narrow, doubl
             constexpr bool V = decltype(v)::value;
             if (!narrow) {
                 constexpr auto kernel = attn_bwd_dq_kernel<E, D, 4, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
+                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
             } else if constexpr (has_narrow<T, D>) {
                 constexpr auto kernel = attn_bwd_dq_kernel<E, D, 1, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
+                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
             }
         });
     }
@@ -101,14 +101,22 @@ template <typename T> hch_status launch_bwd_dkv(const Args &a, bool narrow, doub
             constexpr bool V = decltype(v)::value;
             if (!narrow) {
                 constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 4, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Queries<E, D, 4, V>::THREADS)), 0, s, a);
+                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Queries<E, D, 4, V>::THREADS)), 0, s, a);
             } else if constexpr (has_narrow<T, D>) {
                 constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 1, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a.total)), dim3((Queries<E, D, 1, V>::THREADS)), 0, s, a);
+                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Queries<E, D, 1, V>::THREADS)), 0, s, a);
             }
         });
     }
     HCH_LAUNCH_CHECK("attn_bwd_dkv_kernel");
+    if (a.splits > 1) {
+        {
+            LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_join_keys_kernel"), s, (double)a.splits * a.nk * a.hkv * 8 * a.d, 0.0);
+            constexpr auto kernel = attn_bwd_join_keys_kernel<T>;
+            HCH_LAUNCH(kernel, dim3((unsigned)((2 * a.nk * a.hkv * a.d + 255) / 256)), dim3(256), 0, s, a);
+        }
+        HCH_LAUNCH_CHECK("attn_bwd_join_keys_kernel");
+    }
     return HCH_OK;
 }
 
