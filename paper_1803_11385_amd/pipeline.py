@@ -1,5 +1,5 @@
 """Sequencing of the library calls for a multi-level encoder (conv3x3x3 -> ReLU -> 2x2x2
-max-pool per level) forward and backward.  Only call order and buffer ownership live here;
+max-pool per level) and for an attention block on a level, forward and backward.  Only call order and buffer ownership live here;
 every arithmetic step is a call into libhch.so."""
 from __future__ import annotations
 
@@ -128,3 +128,95 @@ class Encoder:
         self.build_indices()
         self.forward()
         self.backward()
+
+
+class AttentionBlock:
+    """A pre-norm attention block over the voxels of one level, each shape by itself, forward and backward:
+
+        h = norm1(X);  q, k, v = h Wqkv with rotary positions from the voxels;  S = X + attention(q, k, v) Wo;  Y = norm2(S)
+
+    S is the block's result on the residual path, Y what the next layer takes.  X, S, Y and all gradients
+    of them are fp32 [n][channels]; with dtype = HCH_BF16 what goes into products is bf16.  The linear layers are
+    convolutions with F = 1.  `sections`: pairs of a head turned by x, y and z (default: a third each).  All buffers are
+    allocated once here; key_mask (bytes, nonzero = seen) may be set between passes."""
+
+    def __init__(self, levels, level, channels, heads_q, heads_kv, head_dim, dtype=B.HCH_F32, sections=None, base=10000.0,
+                 eps=1e-5, device="cuda"):
+        self.levels, self.level, self.c, self.dtype = levels, level, channels, dtype
+        self.hq, self.hkv, self.d, self.eps, self.base = heads_q, heads_kv, head_dim, eps, base
+        third = head_dim // 6
+        self.sections = (head_dim // 2 - 2 * third, third, third) if sections is None else tuple(sections)
+        self.scale = head_dim ** -0.5
+        n = self.n = levels.n(level)
+        self.wide = (heads_q + 2 * heads_kv) * head_dim
+        wq, wk, c = heads_q * head_dim, heads_kv * head_dim, channels
+        f32 = dict(dtype=torch.float32, device=device)
+        t = dict(dtype=torch.bfloat16 if dtype == B.HCH_BF16 else torch.float32, device=device)
+        self.offsets, self.positions, self.key_mask = levels.device_offsets(level), levels.device_positions(level), None
+        self.field = torch.empty((n, 1), dtype=torch.int32, device=device)
+        self.field_t = torch.empty((n, 1), dtype=torch.int32, device=device)
+        B.hch_field_build(levels, level, 1, 1, 0, self.field, self.field_t)
+        # weights (in the products' type) and their gradients
+        self.gamma, self.beta = [torch.ones(c, **f32) for _ in range(2)], [torch.zeros(c, **f32) for _ in range(2)]
+        self.Wqkv, self.Wo = torch.empty((1, c, self.wide), **t), torch.empty((1, wq, c), **t)
+        self.dgamma, self.dbeta = [torch.empty(c, **f32) for _ in range(2)], [torch.empty(c, **f32) for _ in range(2)]
+        self.dWqkv, self.dWo = torch.empty((1, c, self.wide), **f32), torch.empty((1, wq, c), **f32)
+        # forward
+        self.X, self.S, self.Y, self.P = (torch.empty((n, c), **f32) for _ in range(4))
+        self.h, self.O = torch.empty((n, c), **t), torch.empty((n, wq), **t)
+        self.stats = [torch.empty((n, 2), **f32) for _ in range(2)]
+        self.proj = torch.empty((n, self.wide), **f32)
+        self.qkv = self.proj if dtype == B.HCH_F32 else torch.empty((n, self.wide), **t)
+        self.q, self.k, self.v = self.qkv[:, :wq], self.qkv[:, wq: wq + wk], self.qkv[:, wq + wk:]
+        self.lse = torch.empty((n, heads_q), **f32)
+        # backward; in fp32 the gradients go into products as they are
+        same = dtype == B.HCH_F32
+        self.dY, self.dX, self.dS, self.dh = (torch.empty((n, c), **f32) for _ in range(4))
+        self.dP = self.dS if same else torch.empty((n, c), **t)
+        self.dO32 = torch.empty((n, wq), **f32)
+        self.dO = self.dO32 if same else torch.empty((n, wq), **t)
+        self.dqkv = torch.empty((n, self.wide), **t)
+        self.dq, self.dk, self.dv = self.dqkv[:, :wq], self.dqkv[:, wq: wq + wk], self.dqkv[:, wq + wk:]
+        b = self.offsets.numel() - 1
+        need = [B.hch_layernorm_workspace_bytes(n, c)]
+        need += [B.hch_attn_workspace_bytes(k, dtype, b, n, n, heads_q, heads_kv, head_dim) for k in (B.HCH_WS_FWD, B.HCH_WS_BWD_DATA)]
+        for kind in (B.HCH_WS_FWD, B.HCH_WS_BWD_DATA, B.HCH_WS_BWD_WEIGHT):
+            need += [B.hch_sconv_workspace_bytes(levels, level, 1, 1, ci, co, dtype, kind) for ci, co in ((c, self.wide), (wq, c))]
+        self.ws = _aligned_bytes(max(need), device)
+
+    def _convert(self, x, y):
+        """y = x in the products' type: rotary positions that turn nothing."""
+        if y is not x:
+            w = x.shape[1] // 2
+            B.hch_rope_fwd(B.HCH_F32, x, self.dtype, y, None, self.n, w, 0, 2, (0, 0, 0))
+
+    def forward(self):
+        """X -> S, Y"""
+        n, c, wq, dt, lv = self.n, self.c, self.hq * self.d, self.dtype, (self.levels, self.level, 1, 1)
+        B.hch_layernorm_fwd(B.HCH_F32, self.X, None, None, self.gamma[0], self.beta[0], dt, self.h, self.stats[0], n, c, self.eps)
+        B.hch_sconv_fwd(*lv, dt, self.h, self.Wqkv, self.proj, self.field, c, self.wide, self.ws)
+        B.hch_rope_fwd(B.HCH_F32, self.proj, dt, self.qkv, self.positions, n, self.hq + 2 * self.hkv, self.hq + self.hkv, self.d,
+                       self.sections, self.base)
+        B.hch_attn_fwd(dt, self.q, self.k, self.v, self.O, self.lse, self.offsets, self.offsets, self.key_mask, self.hq, self.hkv,
+                       self.d, self.scale, self.ws)
+        B.hch_sconv_fwd(*lv, dt, self.O, self.Wo, self.P, self.field, wq, c, self.ws)
+        B.hch_layernorm_fwd(B.HCH_F32, self.X, self.P, self.S, self.gamma[1], self.beta[1], B.HCH_F32, self.Y, self.stats[1], n, c,
+                            self.eps)
+
+    def backward(self, dS=None):
+        """dY (and the gradient dS that reaches S by itself) -> dX and the weights' gradients"""
+        n, c, wq, dt, lv = self.n, self.c, self.hq * self.d, self.dtype, (self.levels, self.level, 1, 1)
+        B.hch_layernorm_bwd(B.HCH_F32, self.S, self.stats[1], self.gamma[1], B.HCH_F32, self.dY, dS, self.dS, self.dgamma[1],
+                            self.dbeta[1], n, c, self.ws)
+        self._convert(self.dS, self.dP)
+        B.hch_sconv_bwd_weight(*lv, dt, self.O, self.dP, self.dWo, self.field, wq, c, self.ws)
+        B.hch_sconv_bwd_data(*lv, dt, self.dP, self.Wo, self.dO32, self.field_t, wq, c, self.ws)
+        self._convert(self.dO32, self.dO)
+        B.hch_attn_bwd(dt, self.q, self.k, self.v, self.O, self.lse, self.dO, self.dq, self.dk, self.dv, self.offsets, self.offsets,
+                       self.key_mask, self.hq, self.hkv, self.d, self.scale, self.ws)
+        B.hch_rope_bwd(dt, self.dqkv, dt, self.dqkv, self.positions, n, self.hq + 2 * self.hkv, self.hq + self.hkv, self.d,
+                       self.sections, self.base)
+        B.hch_sconv_bwd_weight(*lv, dt, self.h, self.dqkv, self.dWqkv, self.field, c, self.wide, self.ws)
+        B.hch_sconv_bwd_data(*lv, dt, self.dqkv, self.Wqkv, self.dh, self.field_t, c, self.wide, self.ws)
+        B.hch_layernorm_bwd(B.HCH_F32, self.X, self.stats[0], self.gamma[0], B.HCH_F32, self.dh, self.dS, self.dX, self.dgamma[0],
+                            self.dbeta[0], n, c, self.ws)
