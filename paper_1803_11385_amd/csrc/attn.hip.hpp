@@ -48,6 +48,7 @@ struct Args {
     int batch, hq, hkv, group, d;
     int slots, splits, run, per_head;      // tiles per head at most, splits over the streamed rows; see work_item
     int vec;                               // everything in 16-byte pieces
+    int sorted;                            // units in the order of what streams past them, the longest first
     float scale, c;                        // c = scale log2(e)
 };
 
@@ -198,24 +199,35 @@ __device__ __forceinline__ constexpr int reg_row(int r) { return 8 * (r >> 2) + 
 // ---------------------------------------------------------------------------------------------
 // work distribution
 // ---------------------------------------------------------------------------------------------
-// Workgroups go to the 8 XCDs in turn; runs of `run` neighbours in the work list are kept on one, so that the tiles that
-// read the same keys share its L2, while shapes of different lengths still spread over all of them.  Runs are short where there
-// are few workgroups, or some XCDs would get more than others: 512 of dQ (8 shapes of 2000 rows, 32 channels, fp32) took 108 us
-// in runs of 16 and take 81 one by one.
-// A head's part of the list is a whole number of turns, so that heads that share lines of memory meet on one XCD.
-__device__ __forceinline__ int work_item(int id, int run) { return ((id >> 3) / run * 8 + (id & 7)) * run + (id >> 3) % run; }
+// A unit of work is one split of one tile of one key head.  Where what streams past is long, units of a head are ordered by
+// shape, the longest first, so that a launch ends with its shortest (46514 voxels in 4 shapes, 4 heads of 128, bf16: 1196 -> 1140
+// us; where it is short, finding the order would take longer than it saves); heads alternate.  Workgroups go to the 8 XCDs in turn.  With many units, runs of `run`
+// neighbours of a head are kept on one XCD: they read the same keys, from its L2.  With few, one by one (512 of
+// dQ, 8 shapes of 2000 rows, 32 channels, fp32: 108 us in runs of 16, 81 so), and all heads of a tile on one XCD, since they share
+// lines of memory (8 shapes of 76165 keys, 2 heads of 32, bf16, one query: 47 us apart, 27 together).
 inline void set_work(Args &a)
 {
     const int64_t each = (int64_t)a.slots * a.splits, total = each * a.hkv;
     a.run = total >= 4096 ? 16 : total >= 1024 ? 4 : 1;
-    a.per_head = (int)((each + 8 * a.run - 1) / (8 * a.run) * (8 * a.run));
+    const int whole = a.run == 1 ? 8 : a.run;
+    a.per_head = (int)((each + whole - 1) / whole * whole);
 }
-inline unsigned work_grid(const Args &a) { return (unsigned)a.per_head * (unsigned)a.hkv; }
+inline unsigned work_grid(const Args &a) { return (unsigned)(((int64_t)a.per_head * a.hkv + 8 * a.run - 1) / (8 * a.run) * (8 * a.run)); }
 struct Work { int head, slot, split; };         // slot beyond the last: nothing to do
 __device__ __forceinline__ Work work_of(const Args &a, int id)
 {
-    const int w = work_item(id, a.run), head = w / a.per_head, rest = w - head * a.per_head, slot = rest / a.splits;
-    return {head, slot, rest - slot * a.splits};
+    int head, unit;
+    if (a.run == 1) {
+        const int turn = id >> 3;
+        head = turn % a.hkv;
+        unit = turn / a.hkv * 8 + (id & 7);
+    } else {
+        const int r = (id >> 3) / a.run * 8 + (id & 7);
+        head = r % a.hkv;
+        unit = r / a.hkv * a.run + (id >> 3) % a.run;
+    }
+    const int slot = unit / a.splits;
+    return {head, unit < a.per_head ? slot : a.slots, unit - slot * a.splits};
 }
 
 // A shape's rows [begin, end) of n, safe whatever the offsets hold.
@@ -229,22 +241,47 @@ __device__ __forceinline__ Span span_of(const int32_t *off, int b, int64_t n)
     s.end = max(s.end, s.begin);
     return s;
 }
-// Tiles of `size` rows are dealt to shapes without a sum over them: shape b's tiles have the slots from
-// floor(offset_b / size) + b on, which is room enough, as ceil(len / size) <= floor(end / size) - floor(begin / size) + 1.
-// Returns the shape of a slot (the last whose first slot is not beyond it), by 64-fold search.
-__device__ __forceinline__ int shape_of_slot(const int32_t *off, int batch, int64_t n, int rows_each, int size, int slot, int lane)
+// Where a slot's tile lies: its rows are of `own` (rows_each for each of its shape's), what streams past it of `stream`.
+struct Place { Span own, stream; int tile; };   // tile < 0: there is none
+__device__ __forceinline__ Place place_of(const int32_t *own, int64_t n_own, const int32_t *stream, int64_t n_stream, int batch, bool sorted,
+                                          int rows_each, int size, int slot, int lane)
 {
+    // In the shapes' own order no sum over them is needed: shape b's tiles have the slots from floor(offset_b / size) + b on, which
+    // is room enough, as ceil(len / size) <= floor(end / size) - floor(begin / size) + 1.
+    auto first = [&](int begin, int b) { return (int)((int64_t)begin * rows_each / size) + b; };
+    if (batch <= 64) {                              // a lane per shape
+        const int i = min(lane, batch - 1);
+        const int o0 = clamped(own[i], n_own), o1 = max(o0, clamped(own[i + 1], n_own));
+        const int s0 = clamped(stream[i], n_stream), s1 = max(s0, clamped(stream[i + 1], n_stream));
+        const int tiles = lane < batch ? (int)(((int64_t)(o1 - o0) * rows_each + size - 1) / size) : 0, len = s1 - s0;
+        int before = first(o0, lane);
+        if (sorted) {
+            before = 0;
+            for (int j = 0; j < batch; ++j) {
+                const int tj = __builtin_amdgcn_readlane(tiles, j), lj = __builtin_amdgcn_readlane(len, j);
+                if (lj > len || (lj == len && j < lane)) before += tj;
+            }
+        }
+        const uint64_t hit = __ballot(slot >= before && slot - before < tiles);
+        if (!hit) return {{0, 0}, {0, 0}, -1};
+        const int b = __builtin_ctzll(hit);
+        return {{__builtin_amdgcn_readlane(o0, b), __builtin_amdgcn_readlane(o1, b)}, {__builtin_amdgcn_readlane(s0, b), __builtin_amdgcn_readlane(s1, b)},
+                slot - __builtin_amdgcn_readlane(before, b)};
+    }
+    // more: by 64-fold search
     int lo = 0, cnt = batch;
     while (cnt > 1) {
         const int step = (cnt + 63) >> 6, i = lane * step;
-        const bool in = i < cnt && (int64_t)clamped(off[lo + (i < cnt ? i : 0)], n) * rows_each / size + lo + i <= slot;
+        const bool in = i < cnt && first(clamped(own[lo + (i < cnt ? i : 0)], n_own), lo + i) <= slot;
         const int k = max(0, (int)__popcll(__ballot(in)) - 1);
         lo += k * step;
         cnt = min(step, cnt - k * step);
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const Span o = span_of(own, lo, n_own);
+    const int tile = slot - first(o.begin, lo);
+    return {o, span_of(stream, lo, n_stream), tile >= 0 && (int64_t)tile * size < (int64_t)(o.end - o.begin) * rows_each ? tile : -1};
 }
-__device__ __forceinline__ int first_slot(int begin, int rows_each, int size, int b) { return (int)((int64_t)begin * rows_each / size) + b; }
 inline int64_t slots_of(int64_t n, int rows_each, int size, int batch) { return n * rows_each / size + batch; }
 
 // ---------------------------------------------------------------------------------------------
@@ -293,18 +330,19 @@ template <typename E, int D, int ROWS, int THREADS> struct Stage {
             else r[i] = load_elements<T>(rs, offset, row < rows ? have : 0);
         }
     }
-    // bit `row` of keep[row / 64] clear: the row is written as zeros
-    __device__ __forceinline__ void store(char *tile, int tid, const uint64_t *keep)
+    // rows whose bit of `keep` is clear are written as zeros, unless `all` are to be kept
+    template <int W> __device__ __forceinline__ void store(char *tile, int tid, bool all, const uint64_t (&keep)[W])
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int p = tid + i * THREADS, row = p / PER_ROW, col = p - row * PER_ROW;
             if (PIECES % THREADS && p >= PIECES) continue;
             u32x4 v = r[i];
-            if (keep && !(keep[row >> 6] >> (row & 63) & 1)) v = u32x4{0, 0, 0, 0};
+            if (!all && !((W > 1 && row >= 64 ? keep[W - 1] : keep[0]) >> (row & 63) & 1)) v = u32x4{0, 0, 0, 0};
             E::store(tile + row * Tile<E, D>::STRIDE, ROWS * Tile<E, D>::STRIDE, Layout<D>::swap(row), col, v);
         }
     }
+    __device__ __forceinline__ void store(char *tile, int tid) { store(tile, tid, true, {0ull}); }
 };
 
 // The same without registers, for bf16 in whole pieces: every instruction moves 64 pieces from memory to 1 KB of LDS,
@@ -378,12 +416,12 @@ template <typename E, int D> struct Own {
 // the product that takes it, and wait for it.
 __device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x406); }
 
-// out[i] += (rows 32 i .. of the tile) . own, for N runs of 32 rows.  AHEAD operands are read before the first product, and as
+// out[i] += (rows 32 i .. of the tile) . own, for N runs of 32 rows.  G operands are read before the first product, and as
 // many more while those multiply.
-template <typename E, int D, int N>
+template <typename E, int D, int N, int G = E::AHEAD>
 __device__ __forceinline__ void products(const char *tile, int plane, const Own<E, D> &own, int lane, f32x16 (&out)[N])
 {
-    constexpr int CH = Tile<E, D>::CHUNKS, G = E::AHEAD, TOTAL = N * CH;
+    constexpr int CH = Tile<E, D>::CHUNKS, TOTAL = N * CH;
     const int at = Layout<D>::row0(lane);
     typename E::Part a[2][G];
     auto read = [&](int g) {
@@ -408,8 +446,7 @@ __device__ __forceinline__ void products(const char *tile, int plane, const Own<
 
 // acc[dt] += (rows of a tile, transposed) p, for the channels from `left`'s on, 16 rows at a time.  The first operands are read
 // by the constructor, so that they arrive while p is still being made.
-template <typename E, int D, int DT> struct Fold {
-    static constexpr int G = E::PLANES == 1 ? DT : 1;       // operands read ahead
+template <typename E, int D, int DT, int G = E::PLANES == 1 ? DT : 1> struct Fold {     // G operands read ahead
     typename E::Part a[2][G];
     const char *tile;
     int plane, left;
@@ -471,12 +508,13 @@ __device__ __forceinline__ int key_byte(const uint8_t *mask, int key, int end) {
 template <typename E, int D, int QW, bool VEC> struct Keys {
     static constexpr int WAVES = 4, THREADS = 64 * WAVES, DW = QW == 1 && E::PLANES == 3 && D > 64 ? 2 : 1, KW = WAVES / QW / DW, BQ = 32 * QW;
     static constexpr int DT = D / 32 / DW;                  // of a wavefront's result
+    static constexpr int AHEAD = E::PLANES == 1 && D == 128 ? 2 : E::AHEAD, FOLD = E::PLANES > 1 ? 1 : D == 128 ? 2 : DT;      // of dQ: registers
     static constexpr int BK = QW == 1 ? 32 * KW : E::PLANES == 1 ? 64 : 32, NT = BK / 32 / KW;
     static constexpr int PLANE = BK * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE;
-    static constexpr int BUFFERS = QW == 1 || 4 * TILE > 80 * 1024 ? 1 : 2;     // two where two workgroups still share a compute unit
+    static constexpr int BUFFER = 2 * TILE + 4 * BK, BUFFERS = QW == 1 || 2 * BUFFER > 80 * 1024 ? 1 : 2;   // two where two workgroups still share a compute unit
     static constexpr int WORDS = (BK + 63) / 64;
     static constexpr bool DIRECT = VEC && E::PLANES == 1 && QW == 4;   // two buffers, so the loads of the next tile need no registers
-    static constexpr int JOIN = QW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = 2 * BUFFERS * TILE > JOIN ? 2 * BUFFERS * TILE : JOIN;
+    static constexpr int JOIN = QW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = BUFFERS * BUFFER > JOIN ? BUFFERS * BUFFER : JOIN;
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -496,11 +534,10 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     const Work w = work_of(a, blockIdx.x);
     const int split = w.split, slot = w.slot, kvh = w.head;
     if (slot >= a.slots) return;
-    const int b = shape_of_slot(a.qo, a.batch, a.nq, a.group, S::BQ, slot, lane);
-    const Span q = span_of(a.qo, b, a.nq), k = span_of(a.ko, b, a.nk);
-    const int tile = slot - first_slot(q.begin, a.group, S::BQ, b);
-    const int64_t rows = (int64_t)(q.end - q.begin) * a.group, row0 = (int64_t)tile * S::BQ;
-    if (tile < 0 || row0 >= rows) return;
+    const Place place = place_of(a.qo, a.nq, a.ko, a.nk, a.batch, a.sorted, a.group, S::BQ, slot, lane);
+    if (place.tile < 0) return;
+    const Span q = place.own, k = place.stream;
+    const int64_t rows = (int64_t)(q.end - q.begin) * a.group, row0 = (int64_t)place.tile * S::BQ;
 
     const int64_t row = row0 + 32 * qw + (lane & 31);
     const bool valid = row < rows;
@@ -526,7 +563,7 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     typedef Direct<D, S::BK> Dir;
     Regs ks, vs;
     int seen[S::WORDS];
-    auto buffer = [&](int t) { return lds + (S::BUFFERS == 2 ? (t & 1) * 2 * S::TILE : 0); };
+    auto buffer = [&](int t) { return lds + (S::BUFFERS == 2 ? (t & 1) * S::BUFFER : 0); };
     auto load = [&](int t) {
         if constexpr (S::DIRECT) {
             Dir::load(kp, a.ld_k, t * S::BK, len, a.d, buffer(t), wave, lane);
@@ -538,24 +575,9 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
 #pragma unroll
         for (int i = 0; i < S::WORDS; ++i) seen[i] = key_byte(mask, t * S::BK + 64 * i + lane, len);
     };
-    // tile t in LDS; keys that are not seen as zeros in the second matrix (0 * NaN), and where asked for in the first
-    auto arrive = [&](int t, const uint64_t *keep, bool all, bool both) {
-        char *kt = buffer(t), *vt = kt + S::TILE;
-        if constexpr (S::DIRECT) {
-            Dir::wait();
-            if (!all) {
-                Dir::clear(vt, wave, lane, keep[0]);
-                if (both) Dir::clear(kt, wave, lane, keep[0]);
-            }
-        } else {
-            if (S::BUFFERS == 1) __syncthreads();
-            ks.store(kt, tid, all || !both ? nullptr : keep);
-            vs.store(vt, tid, all ? nullptr : keep);
-        }
-        __syncthreads();
-    };
-    if (t0 < t1) load(t0);
-    for (int t = t0; t < t1; ++t) {
+    // Tile t in LDS, keys that are not seen as zeros (they may hold anything, and 0 * NaN is NaN); behind it what the scores of its
+    // keys start from: 0, or -inf for a key that is not seen.
+    auto arrive = [&](int t) {
         char *kt = buffer(t), *vt = kt + S::TILE;
         uint64_t keep[S::WORDS];
         bool all = true;
@@ -564,22 +586,45 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
             keep[i] = __ballot(seen[i] != 0);
             all &= S::BK - 64 * i >= 64 ? keep[i] == ~0ull : (uint32_t)keep[i] == ~0u;
         }
-        arrive(t, keep, all, false);
+        if constexpr (S::DIRECT) {
+            Dir::wait();
+            if (!all) {
+                Dir::clear(vt, wave, lane, keep[0]);
+                Dir::clear(kt, wave, lane, keep[0]);
+            }
+        } else {
+            if (S::BUFFERS == 1) __syncthreads();
+            ks.store(kt, tid, all, keep);
+            vs.store(vt, tid, all, keep);
+        }
+#pragma unroll
+        for (int i = 0; i < S::WORDS; ++i)
+            if (wave == i && 64 * i + lane < S::BK) ((float *)(kt + 2 * S::TILE))[64 * i + lane] = seen[i] ? 0.f : -INFINITY;
+        __syncthreads();
+    };
+    auto start = [&](int t, int run) {
+        f32x16 s;
+        const float *p = (const float *)(buffer(t) + 2 * S::TILE) + 32 * run + 4 * h;
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 x = *(const f32x4 *)(p + reg_row(r));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[r + j] = x[j];
+        }
+        return s;
+    };
+    if (t0 < t1) load(t0);
+    for (int t = t0; t < t1; ++t) {
+        char *kt = buffer(t), *vt = kt + S::TILE;
+        arrive(t);
         if (t + 1 < t1) load(t + 1);
 
         const int sub = QW == 1 ? kw : 0;               // the first of this wavefront's runs of 32 keys
         f32x16 s[S::NT];
 #pragma unroll
-        for (int i = 0; i < S::NT; ++i) s[i] = f32x16{};
+        for (int i = 0; i < S::NT; ++i) s[i] = start(t, sub + i);
         products<E, D, S::NT>(kt + 32 * sub * L::STRIDE, S::PLANE, own, lane, s);
         Fold<E, D, S::DT> fold(vt + 32 * sub * L::STRIDE, S::PLANE, left);
-        if (!all)
-#pragma unroll
-            for (int i = 0; i < S::NT; ++i) {
-                const uint32_t bits = (uint32_t)(keep[(sub + i) >> 1] >> (32 * ((sub + i) & 1))) >> (4 * h);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) if (!(bits >> reg_row(r) & 1)) s[i][r] = -INFINITY;
-            }
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < S::NT; ++i)
@@ -796,11 +841,10 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     const Work w = work_of(a, blockIdx.x);
     const int split = w.split, slot = w.slot, kvh = w.head;
     if (slot >= a.slots) return;
-    const int b = shape_of_slot(a.qo, a.batch, a.nq, a.group, S::BQ, slot, lane);
-    const Span q = span_of(a.qo, b, a.nq), k = span_of(a.ko, b, a.nk);
-    const int tile = slot - first_slot(q.begin, a.group, S::BQ, b);
-    const int64_t rows = (int64_t)(q.end - q.begin) * a.group, row0 = (int64_t)tile * S::BQ;
-    if (tile < 0 || row0 >= rows) return;
+    const Place place = place_of(a.qo, a.nq, a.ko, a.nk, a.batch, a.sorted, a.group, S::BQ, slot, lane);
+    if (place.tile < 0) return;
+    const Span q = place.own, k = place.stream;
+    const int64_t rows = (int64_t)(q.end - q.begin) * a.group, row0 = (int64_t)place.tile * S::BQ;
 
     const int64_t row = row0 + 32 * qw + (lane & 31);
     const bool valid = row < rows;
@@ -832,7 +876,7 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     typedef Direct<D, S::BK> Dir;
     Regs ks, vs;
     int seen[S::WORDS];
-    auto buffer = [&](int t) { return lds + (S::BUFFERS == 2 ? (t & 1) * 2 * S::TILE : 0); };
+    auto buffer = [&](int t) { return lds + (S::BUFFERS == 2 ? (t & 1) * S::BUFFER : 0); };
     auto load = [&](int t) {
         if constexpr (S::DIRECT) {
             Dir::load(kp, a.ld_k, t * S::BK, len, a.d, buffer(t), wave, lane);
@@ -844,24 +888,9 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
 #pragma unroll
         for (int i = 0; i < S::WORDS; ++i) seen[i] = key_byte(mask, t * S::BK + 64 * i + lane, len);
     };
-    // tile t in LDS; keys that are not seen as zeros in the second matrix (0 * NaN), and where asked for in the first
-    auto arrive = [&](int t, const uint64_t *keep, bool all, bool both) {
-        char *kt = buffer(t), *vt = kt + S::TILE;
-        if constexpr (S::DIRECT) {
-            Dir::wait();
-            if (!all) {
-                Dir::clear(vt, wave, lane, keep[0]);
-                if (both) Dir::clear(kt, wave, lane, keep[0]);
-            }
-        } else {
-            if (S::BUFFERS == 1) __syncthreads();
-            ks.store(kt, tid, all || !both ? nullptr : keep);
-            vs.store(vt, tid, all ? nullptr : keep);
-        }
-        __syncthreads();
-    };
-    if (t0 < t1) load(t0);
-    for (int t = t0; t < t1; ++t) {
+    // Tile t in LDS, keys that are not seen as zeros (they may hold anything, and 0 * NaN is NaN); behind it what the scores of its
+    // keys start from: 0, or -inf for a key that is not seen.
+    auto arrive = [&](int t) {
         char *kt = buffer(t), *vt = kt + S::TILE;
         uint64_t keep[S::WORDS];
         bool all = true;
@@ -870,22 +899,47 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
             keep[i] = __ballot(seen[i] != 0);
             all &= S::BK - 64 * i >= 64 ? keep[i] == ~0ull : (uint32_t)keep[i] == ~0u;
         }
-        arrive(t, keep, all, true);
+        if constexpr (S::DIRECT) {
+            Dir::wait();
+            if (!all) {
+                Dir::clear(vt, wave, lane, keep[0]);
+                Dir::clear(kt, wave, lane, keep[0]);
+            }
+        } else {
+            if (S::BUFFERS == 1) __syncthreads();
+            ks.store(kt, tid, all, keep);
+            vs.store(vt, tid, all, keep);
+        }
+#pragma unroll
+        for (int i = 0; i < S::WORDS; ++i)
+            if (wave == i && 64 * i + lane < S::BK) ((float *)(kt + 2 * S::TILE))[64 * i + lane] = seen[i] ? 0.f : -INFINITY;
+        __syncthreads();
+    };
+    auto start = [&](int t, int run) {
+        f32x16 s;
+        const float *p = (const float *)(buffer(t) + 2 * S::TILE) + 32 * run + 4 * h;
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const f32x4 x = *(const f32x4 *)(p + reg_row(r));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[r + j] = x[j];
+        }
+        return s;
+    };
+    if (t0 < t1) load(t0);
+    for (int t = t0; t < t1; ++t) {
+        char *kt = buffer(t), *vt = kt + S::TILE;
+        arrive(t);
         if (t + 1 < t1) load(t + 1);
 #pragma unroll
         for (int i = 0; i < S::NT; ++i) {
             const int sub = QW == 1 ? kw : i;
-            f32x16 s[1] = {f32x16{}}, g[1];
+            f32x16 s[1] = {start(t, sub)}, g[1];
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[0][r] = -delta;
-            products<E, D, 1>(kt + 32 * sub * L::STRIDE, S::PLANE, own, lane, s);
-            products<E, D, 1>(vt + 32 * sub * L::STRIDE, S::PLANE, grad, lane, g);
-            Fold<E, D, S::DT> fold(kt + 32 * sub * L::STRIDE, S::PLANE, left);
-            if (!all) {
-                const uint32_t bits = (uint32_t)(keep[sub >> 1] >> (32 * (sub & 1))) >> (4 * h);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) if (!(bits >> reg_row(r) & 1)) s[0][r] = -INFINITY;
-            }
+            products<E, D, 1, S::AHEAD>(kt + 32 * sub * L::STRIDE, S::PLANE, own, lane, s);
+            products<E, D, 1, S::AHEAD>(vt + 32 * sub * L::STRIDE, S::PLANE, grad, lane, g);
+            Fold<E, D, S::DT, S::FOLD> fold(kt + 32 * sub * L::STRIDE, S::PLANE, left);
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[0][r] *= exp2_fast(__builtin_fmaf(s[0][r], a.c, -lse2));
             fold.run(g, acc);
@@ -936,12 +990,11 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
     const Work w = work_of(a, blockIdx.x);
     const int split = w.split, slot = w.slot, kvh = w.head;
     if (slot >= a.slots) return;
-    const int b = shape_of_slot(a.ko, a.batch, a.nk, 1, S::BK, slot, lane);
-    const Span q = span_of(a.qo, b, a.nq), k = span_of(a.ko, b, a.nk);
-    const int tile = slot - first_slot(k.begin, 1, S::BK, b);
-    if (tile < 0 || tile >= (k.end - k.begin + S::BK - 1) / S::BK) return;
+    const Place place = place_of(a.ko, a.nk, a.qo, a.nq, a.batch, a.sorted, 1, S::BK, slot, lane);
+    if (place.tile < 0) return;
+    const Span q = place.stream, k = place.own;
 
-    const int64_t key = k.begin + (int64_t)tile * S::BK + 32 * kw + (lane & 31);
+    const int64_t key = k.begin + (int64_t)place.tile * S::BK + 32 * kw + (lane & 31);
     const bool valid = key < k.end, seen = valid && (!a.mask || a.mask[key]);
     Own<E, D> kk, vv;
     kk.load((const T *)a.K + (valid ? key : 0) * a.ld_k + (int64_t)kvh * a.d, seen, a.d, VEC, h);
@@ -984,8 +1037,8 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
             Dir::wait();
         } else {
             if (S::BUFFERS == 1) __syncthreads();
-            qs.store(qt, tid, nullptr);
-            gs.store(gt, tid, nullptr);
+            qs.store(qt, tid);
+            gs.store(gt, tid);
         }
         if (tid < S::BR) {
             stat[tid] = lse == -INFINITY ? -INFINITY : -lse * LOG2E;    // no such row, or one that saw no key: p = 0

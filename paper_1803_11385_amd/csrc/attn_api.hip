@@ -42,10 +42,11 @@ Plan plan(const hch_attn_desc &p, int64_t rows, int heads, double stream, double
         const Step &st = STEP[type][narrow][dc];
         const int size = narrow ? 32 : 128, step = narrow ? (!type && dc >= 2 ? 64 : 128) : type ? 64 : 32;
         const double wgs = std::max<double>(p.batch, (double)rows / size + 0.5 * p.batch) * heads, steps = std::max(1.0, std::ceil(stream / step));
-        // one to three splits, and as many as make whole rounds of workgroups
-        for (int i = 1; i <= 9; ++i) {
-            const int splits = i <= 3 ? i : (int)std::min(256.0, UNITS * (i - 3) / wgs);
-            if (splits < 1 || splits > steps) continue;
+        // half as many again from time to time, and as many as make whole rounds of workgroups
+        constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}, COUNT = sizeof(SPLITS) / sizeof(int);
+        for (int i = 0; i < COUNT + 4; ++i) {
+            const int splits = i < COUNT ? SPLITS[i] : (int)std::min(256.0, UNITS * (i - COUNT + 1) / wgs);
+            if (splits < 1 || splits > steps || (splits > 1 && wgs * splits > 4 * UNITS)) continue;
             const double each = std::ceil(wgs * splits / UNITS), busy = each <= 1.0 ? 1.0 : std::max(1.0, each / st.at_once);
             double us = (START + std::ceil(UNEVEN * steps / splits) * st.us * cost) * busy;
             // Memory: at its rate if the compute units share evenly, and not with more than two workgroups each at it (8 shapes
@@ -129,9 +130,12 @@ hch_status check_call(const char *who, const hch_attn_desc *p, const void *works
     return HCH_OK;
 }
 
+constexpr int64_t SORT_FROM = 1024;                     // keys of a shape
+
 Args args_of(const hch_attn_desc &p)
 {
     Args a = {};
+    a.sorted = p.batch > 1 && p.n_k / std::max(1, p.batch) >= SORT_FROM;
     a.qo = p.q_offsets; a.ko = p.k_offsets; a.mask = p.key_mask;
     a.nq = p.n_q; a.nk = p.n_k;
     a.ld_q = p.ld_q; a.ld_k = p.ld_k; a.ld_v = p.ld_v; a.ld_o = p.ld_o;
