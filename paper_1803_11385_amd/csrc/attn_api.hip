@@ -85,48 +85,38 @@ size_t ml_bytes(const hch_attn_desc &p, int splits) { return splits > 1 ? round2
 size_t key_part_bytes(const hch_attn_desc &p, int splits) { return splits > 1 ? round256((size_t)splits * p.n_k * p.heads_kv * p.head_dim * 8) : 0; }
 size_t delta_bytes(const hch_attn_desc &p) { return round256((size_t)p.n_q * p.heads_q * 4); }
 
-size_t fwd_bytes(const hch_attn_desc &p)
+size_t fwd_bytes(const hch_attn_desc &p, const Plan &r) { return std::max<size_t>(256, part_bytes(p, r.splits) + ml_bytes(p, r.splits)); }
+// the parts of dQ are joined before those of dK and dV are written
+size_t bwd_bytes(const hch_attn_desc &p, const Plan &dq, const Plan &dkv)
 {
-    if (!p.batch || !p.n_q) return 256;
-    const Plan r = plan_keys(p, FWD);
-    return std::max<size_t>(256, part_bytes(p, r.splits) + ml_bytes(p, r.splits));
-}
-size_t bwd_bytes(const hch_attn_desc &p)            // the parts of dQ are joined before those of dK and dV are written
-{
-    if (!p.batch || !p.n_q) return 256;
-    return delta_bytes(p) + std::max<size_t>({256, part_bytes(p, plan_keys(p, DQ).splits), key_part_bytes(p, plan_queries(p).splits)});
+    return delta_bytes(p) + std::max<size_t>({256, part_bytes(p, dq.splits), key_part_bytes(p, dkv.splits)});
 }
 
 // what both calls and the size query ask of the sizes
 hch_status check_sizes(const char *who, const hch_attn_desc *p)
 {
-    const std::string name = who;
-    if (!p) return fail(HCH_EINVAL, name + ": null description");
-    if (p->dtype != HCH_F32 && p->dtype != HCH_BF16) return fail(HCH_EINVAL, name + ": unknown dtype");
+    const auto no = [&](hch_status st, const char *what) { return fail(st, std::string(who) + what); };
+    if (!p) return no(HCH_EINVAL, ": null description");
+    if (p->dtype != HCH_F32 && p->dtype != HCH_BF16) return no(HCH_EINVAL, ": unknown dtype");
     if (p->batch < 0 || p->n_q < 0 || p->n_k < 0 || p->heads_q <= 0 || p->heads_kv <= 0 || p->head_dim <= 0 || p->heads_q % p->heads_kv)
-        return fail(HCH_EINVAL, name + ": bad size, or heads_q not a multiple of heads_kv");
-    if (p->head_dim > 128) return fail(HCH_EUNSUPPORTED, name + ": more than 128 channels per head");
-    if (p->n_k > 0x7fffffff || p->n_q > 0x7fffffff / p->heads_q) return fail(HCH_EUNSUPPORTED, name + ": more than 2^31 - 1 rows");
-    if (p->batch == 0 && (p->n_q || p->n_k)) return fail(HCH_EINVAL, name + ": rows without a shape");
-    const int64_t group = p->heads_q / p->heads_kv;
-    if (p->batch) {
-        const Plan a = plan_keys(*p, FWD), b = plan_queries(*p), c = plan_keys(*p, DQ);
-        if (std::max({a.slots * a.splits, b.slots * b.splits, c.slots * c.splits}) > 0x7fffffff / p->heads_kv - 256 || group > 0x7fff)
-            return fail(HCH_EUNSUPPORTED, name + ": too many rows for one launch");
-    }
+        return no(HCH_EINVAL, ": bad size, or heads_q not a multiple of heads_kv");
+    if (p->head_dim > 128) return no(HCH_EUNSUPPORTED, ": more than 128 channels per head");
+    if (p->n_k > 0x7fffffff || p->n_q > 0x7fffffff / p->heads_q || p->heads_q > 0x7fff) return no(HCH_EUNSUPPORTED, ": more than 2^31 - 1 rows, or 2^15 - 1 heads");
+    if (p->batch == 0 && (p->n_q || p->n_k)) return no(HCH_EINVAL, ": rows without a shape");
     return HCH_OK;
 }
+bool launchable(const hch_attn_desc &p, const Plan &r) { return r.slots * r.splits <= 0x7fffffff / p.heads_kv - 256; }
 
 hch_status check_call(const char *who, const hch_attn_desc *p, const void *workspace, size_t ws_bytes, size_t need)
 {
-    const std::string name = who;
-    if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return fail(HCH_EINVAL, name + ": scale must be positive and finite");
-    if (p->batch && (!p->q_offsets || !p->k_offsets)) return fail(HCH_EINVAL, name + ": null offsets");
+    const auto no = [&](hch_status st, const char *what) { return fail(st, std::string(who) + what); };
+    if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return no(HCH_EINVAL, ": scale must be positive and finite");
+    if (p->batch && (!p->q_offsets || !p->k_offsets)) return no(HCH_EINVAL, ": null offsets");
     const int64_t wq = (int64_t)p->heads_q * p->head_dim, wk = (int64_t)p->heads_kv * p->head_dim;
-    if (p->ld_q < wq || p->ld_o < wq || p->ld_k < wk || p->ld_v < wk) return fail(HCH_EINVAL, name + ": row stride below a row's length");
-    if (std::max({p->ld_q, p->ld_o, p->ld_k, p->ld_v}) >= 1 << 22) return fail(HCH_EUNSUPPORTED, name + ": row stride of 2^22 elements or more");
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return fail(HCH_EINVAL, name + ": workspace null or not 256-byte aligned");
-    if (ws_bytes < need) return fail(HCH_EWORKSPACE, name + ": workspace too small");
+    if (p->ld_q < wq || p->ld_o < wq || p->ld_k < wk || p->ld_v < wk) return no(HCH_EINVAL, ": row stride below a row's length");
+    if (std::max({p->ld_q, p->ld_o, p->ld_k, p->ld_v}) >= 1 << 22) return no(HCH_EUNSUPPORTED, ": row stride of 2^22 elements or more");
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255)) return no(HCH_EINVAL, ": workspace null or not 256-byte aligned");
+    if (ws_bytes < need) return no(HCH_EWORKSPACE, ": workspace too small");
     return HCH_OK;
 }
 
@@ -162,22 +152,23 @@ double pairs(const hch_attn_desc &p) { return (double)p.n_q * p.n_k / std::max(1
 
 extern "C" size_t hch_attn_workspace_bytes(const hch_attn_desc *desc, hch_ws_kind kind)
 {
-    if (check_sizes("hch_attn_workspace_bytes", desc) != HCH_OK) return 0;
-    if (kind == HCH_WS_FWD) return fwd_bytes(*desc);
-    if (kind == HCH_WS_BWD_DATA) return bwd_bytes(*desc);
-    return 0;
+    if (check_sizes("hch_attn_workspace_bytes", desc) != HCH_OK || (kind != HCH_WS_FWD && kind != HCH_WS_BWD_DATA)) return 0;
+    if (!desc->n_q) return 256;
+    return kind == HCH_WS_FWD ? fwd_bytes(*desc, plan_keys(*desc, FWD)) : bwd_bytes(*desc, plan_keys(*desc, DQ), plan_queries(*desc));
 }
 
 extern "C" hch_status hch_attn_fwd(const hch_attn_desc *desc, const void *Q, const void *K, const void *V, void *O, float *lse,
                                    void *workspace, size_t ws_bytes, void *stream)
 {
     hch_status st = check_sizes("hch_attn_fwd", desc);
-    if (st == HCH_OK) st = check_call("hch_attn_fwd", desc, workspace, ws_bytes, fwd_bytes(*desc));
     if (st != HCH_OK) return st;
     const hch_attn_desc &p = *desc;
+    const Plan r = p.n_q ? plan_keys(p, FWD) : Plan{false, 1, 0};
+    st = check_call("hch_attn_fwd", desc, workspace, ws_bytes, fwd_bytes(p, r));
+    if (st != HCH_OK) return st;
     if ((p.n_q && (!Q || !O)) || (p.n_k && (!K || !V))) return fail(HCH_EINVAL, "hch_attn_fwd: null pointer");
+    if (!launchable(p, r)) return fail(HCH_EUNSUPPORTED, "hch_attn_fwd: too many rows for one launch");
     if (!p.n_q) return HCH_OK;
-    const Plan r = plan_keys(p, FWD);
     Args a = args_of(p);
     a.Q = Q; a.K = K; a.V = V; a.Ow = O; a.lse = lse;
     a.vec = whole(p, {Q, K, V, O}, {p.ld_q, p.ld_k, p.ld_v, p.ld_o});
@@ -193,34 +184,35 @@ extern "C" hch_status hch_attn_bwd(const hch_attn_desc *desc, const void *Q, con
                                    const void *dO, void *dQ, void *dK, void *dV, void *workspace, size_t ws_bytes, void *stream)
 {
     hch_status st = check_sizes("hch_attn_bwd", desc);
-    if (st == HCH_OK) st = check_call("hch_attn_bwd", desc, workspace, ws_bytes, bwd_bytes(*desc));
     if (st != HCH_OK) return st;
     const hch_attn_desc &p = *desc;
+    const Plan none = {false, 1, p.batch ? hch::attn::slots_of(p.n_k, 1, 128, p.batch) : 0};       // without queries: zeros
+    const Plan rq = p.n_q ? plan_keys(p, DQ) : none, rk = p.n_q ? plan_queries(p) : none;
+    st = check_call("hch_attn_bwd", desc, workspace, ws_bytes, p.n_q ? bwd_bytes(p, rq, rk) : 256);
+    if (st != HCH_OK) return st;
     const int64_t wq = (int64_t)p.heads_q * p.head_dim, wk = (int64_t)p.heads_kv * p.head_dim;
     if (p.ld_do < wq || p.ld_dq < wq || p.ld_dk < wk || p.ld_dv < wk) return fail(HCH_EINVAL, "hch_attn_bwd: row stride below a row's length");
     if (std::max({p.ld_do, p.ld_dq, p.ld_dk, p.ld_dv}) >= 1 << 22) return fail(HCH_EUNSUPPORTED, "hch_attn_bwd: row stride of 2^22 elements or more");
     if ((p.n_q && (!Q || !O || !lse || !dO || !dQ)) || (p.n_k && (!K || !V || !dK || !dV))) return fail(HCH_EINVAL, "hch_attn_bwd: null pointer");
+    if (!launchable(p, rq) || !launchable(p, rk)) return fail(HCH_EUNSUPPORTED, "hch_attn_bwd: too many rows for one launch");
     Args a = args_of(p);
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse = const_cast<float *>(lse); a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV;
     a.vec = whole(p, {Q, K, V, O, dO, dQ, dK, dV}, {p.ld_q, p.ld_k, p.ld_v, p.ld_o, p.ld_do, p.ld_dq, p.ld_dk, p.ld_dv});
+    a.delta = (float *)workspace;
+    a.part = (float *)((char *)workspace + delta_bytes(p));
     const hipStream_t s = (hipStream_t)stream;
     if (p.n_q) {
-        const Plan r = plan_keys(p, DQ);
-        a.slots = (int)r.slots; a.splits = r.splits; hch::attn::set_work(a);
-        a.delta = (float *)workspace;
-        a.part = (float *)((char *)workspace + delta_bytes(p));
+        a.slots = (int)rq.slots; a.splits = rq.splits; hch::attn::set_work(a);
         const double bytes = row_bytes(p, 4, 2), flops = 6 * pairs(p);
-        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dq<float>(a, r.narrow, bytes, flops, s)
-                                : hch::attn::launch_bwd_dq<__bf16>(a, r.narrow, bytes, flops, s);
+        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dq<float>(a, rq.narrow, bytes, flops, s)
+                                : hch::attn::launch_bwd_dq<__bf16>(a, rq.narrow, bytes, flops, s);
         if (st != HCH_OK) return st;
     }
     if (p.n_k) {
-        const Plan r = p.n_q ? plan_queries(p) : Plan{false, 1, hch::attn::slots_of(p.n_k, 1, 128, p.batch)};
-        a.slots = (int)r.slots; a.splits = r.splits; hch::attn::set_work(a);
-        a.part = (float *)((char *)workspace + delta_bytes(p));
+        a.slots = (int)rk.slots; a.splits = rk.splits; hch::attn::set_work(a);
         const double bytes = row_bytes(p, 2, 4), flops = 8 * pairs(p);
-        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dkv<float>(a, r.narrow, bytes, flops, s)
-                                : hch::attn::launch_bwd_dkv<__bf16>(a, r.narrow, bytes, flops, s);
+        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dkv<float>(a, rk.narrow, bytes, flops, s)
+                                : hch::attn::launch_bwd_dkv<__bf16>(a, rk.narrow, bytes, flops, s);
     }
     return st;
 }
