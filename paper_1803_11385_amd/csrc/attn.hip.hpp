@@ -543,9 +543,6 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     const bool valid = row < rows;
     const int64_t token = valid ? q.begin + row / a.group : q.begin;
     const int head = kvh * a.group + (valid ? (int)(row % a.group) : 0);
-    Own<E, D> own;
-    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, valid, a.d, VEC, h);
-
     const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
     const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
@@ -613,7 +610,9 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
         }
         return s;
     };
-    if (t0 < t1) load(t0);
+    if (t0 < t1) load(t0);                              // before the own rows, so that neither waits for the other
+    Own<E, D> own;
+    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, valid, a.d, VEC, h);
     for (int t = t0; t < t1; ++t) {
         char *kt = buffer(t), *vt = kt + S::TILE;
         arrive(t);
@@ -851,16 +850,6 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     const int64_t token = valid ? q.begin + row / a.group : q.begin;
     const int head = kvh * a.group + (valid ? (int)(row % a.group) : 0);
     const int64_t at = token * a.hq + head;
-    const float lse = a.lse[at];
-    const bool part = valid && lse != -INFINITY;        // a row that saw no key: its gradient is zero, whatever dO holds
-    const float lse2 = part ? lse * LOG2E : INFINITY;
-    Own<E, D> own, grad;
-    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, part, a.d, VEC, h);
-    grad.load((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d, part, a.d, VEC, h);
-    const float delta = row_dot<T, D>((const T *)a.dO + token * a.ld_do + (int64_t)head * a.d,
-                                      (const T *)a.O + token * a.ld_o + (int64_t)head * a.d, part, a.d, VEC, h);
-    if (valid && split == 0 && kw == 0 && dw == 0 && h == 0) a.delta[at] = delta;
-
     const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
     const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
@@ -927,6 +916,16 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
         return s;
     };
     if (t0 < t1) load(t0);
+    const float lse = a.lse[at];
+    const bool part = valid && lse != -INFINITY;        // a row that saw no key: its gradient is zero, whatever dO holds
+    const float lse2 = part ? lse * LOG2E : INFINITY;
+    Own<E, D> own, grad;
+    const T *gp = (const T *)a.dO + token * a.ld_do + (int64_t)head * a.d;
+    own.load((const T *)a.Q + token * a.ld_q + (int64_t)head * a.d, valid, a.d, VEC, h);
+    grad.load(gp, valid, a.d, VEC, h);
+    float delta = row_dot<T, D>(gp, (const T *)a.O + token * a.ld_o + (int64_t)head * a.d, valid, a.d, VEC, h);
+    if (!part) delta = 0.f;
+    if (valid && split == 0 && kw == 0 && dw == 0 && h == 0) a.delta[at] = delta;
     for (int t = t0; t < t1; ++t) {
         char *kt = buffer(t), *vt = kt + S::TILE;
         arrive(t);
@@ -950,6 +949,9 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
         if (kw) return;
     }
     if (!valid) return;
+    if (!part)
+#pragma unroll
+        for (int dt = 0; dt < S::DT; ++dt) acc[dt] = f32x16{};
     const int e0 = 32 * S::DT * dw;
     if (a.splits == 1) store_row<T>((T *)a.dQ + token * a.ld_dq + (int64_t)head * a.d + e0, acc, a.scale, a.d - e0, VEC, h);
     else store_row<float>(a.part + ((int64_t)split * a.nq * a.hq + at) * a.d + e0, acc, a.scale, a.d - e0, a.d % 4 == 0, h);
@@ -996,10 +998,6 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
 
     const int64_t key = k.begin + (int64_t)place.tile * S::BK + 32 * kw + (lane & 31);
     const bool valid = key < k.end, seen = valid && (!a.mask || a.mask[key]);
-    Own<E, D> kk, vv;
-    kk.load((const T *)a.K + (valid ? key : 0) * a.ld_k + (int64_t)kvh * a.d, seen, a.d, VEC, h);
-    vv.load((const T *)a.V + (valid ? key : 0) * a.ld_v + (int64_t)kvh * a.d, seen, a.d, VEC, h);
-
     const int len = q.end - q.begin, tiles = (len + S::BR - 1) / S::BR;
     const int s0 = (int)((int64_t)tiles * a.group * split / a.splits), s1 = (int)((int64_t)tiles * a.group * (split + 1) / a.splits);
     const int left = Layout<D>::left(Layout<D>::left0(lane), S::DT * dw);
@@ -1030,6 +1028,9 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
     };
     int head = kvh * a.group + (s0 < s1 ? s0 / tiles : 0), t = s0 < s1 ? s0 % tiles : 0;
     if (s0 < s1) load(s0, head, t);
+    Own<E, D> kk, vv;
+    kk.load((const T *)a.K + (valid ? key : 0) * a.ld_k + (int64_t)kvh * a.d, seen, a.d, VEC, h);
+    vv.load((const T *)a.V + (valid ? key : 0) * a.ld_v + (int64_t)kvh * a.d, seen, a.d, VEC, h);
     for (int step = s0; step < s1; ++step) {
         char *qt = buffer(step), *gt = qt + S::TILE;
         float *stat = (float *)(gt + S::TILE);
