@@ -2,7 +2,7 @@
 //   forward   s = x + r;  mu = mean(s);  v = mean((s - mu)^2);  y = (s - mu) / sqrt(v + eps) * gamma + beta
 //   backward  h = (x - mu) rs;  w = dy gamma;  dx = rs (w - mean(w) - h mean(w h)) + ds
 //             dgamma = sum over rows of dy h;  dbeta = sum over rows of dy
-// A row is held by LPR lanes, NV vectors of 4 channels each, and read once: mean and variance come from the
+// A row is held by LPR lanes, NV vectors of W channels each, and read once: mean and variance come from the
 // registers (two passes over them, so a row with a large mean loses nothing), all sums in fp32.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -14,9 +14,7 @@ namespace norm {
 
 constexpr int THREADS = 256;
 
-template <typename T> struct Vec4;
-template <> struct Vec4<float> { typedef float type __attribute__((ext_vector_type(4))); };
-template <> struct Vec4<__bf16> { typedef __bf16 type __attribute__((ext_vector_type(4))); };
+template <typename T, int W> struct Vec { typedef T type __attribute__((ext_vector_type(W))); };
 
 // the sum over a group of LPR lanes (4 .. 64), in every lane of the group; a fixed order
 template <int CTRL> __device__ __forceinline__ float dpp_add(float v)
@@ -53,56 +51,56 @@ template <int LPR> __device__ __forceinline__ float row_sum(float v, float *lds,
     }
 }
 
-// Channel of element j of vector v of a lane.  VEC: 4 neighbours per lane; otherwise the lanes side by side, so that
+// Channel of element j of vector v of a lane.  VEC: W neighbours per lane; otherwise the lanes side by side, so that
 // element by element a wavefront still reads runs.
-template <int LPR, bool VEC> __device__ __forceinline__ int channel(int lane, int v, int j)
+template <int LPR, int W, bool VEC> __device__ __forceinline__ int channel(int lane, int v, int j)
 {
-    return VEC ? (v * LPR + lane) * 4 + j : (v * 4 + j) * LPR + lane;
+    return VEC ? (v * LPR + lane) * W + j : (v * W + j) * LPR + lane;
 }
-template <typename T, int LPR, int NV, bool VEC>
-__device__ __forceinline__ void load_row(const T *row, int lane, int c, float (&x)[4 * NV])
+template <typename T, int LPR, int W, int NV, bool VEC>
+__device__ __forceinline__ void load_row(const T *row, int lane, int c, float (&x)[W * NV])
 {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         if constexpr (VEC) {
-            const int e = channel<LPR, VEC>(lane, v, 0);
-            typename Vec4<T>::type t = {};
-            if (e < c) t = *(const typename Vec4<T>::type *)(row + e);
+            const int e = channel<LPR, W, VEC>(lane, v, 0);
+            typename Vec<T, W>::type t = {};
+            if (e < c) t = *(const typename Vec<T, W>::type *)(row + e);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[4 * v + j] = (float)t[j];
+            for (int j = 0; j < W; ++j) x[W * v + j] = (float)t[j];
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int e = channel<LPR, VEC>(lane, v, j);
-                x[4 * v + j] = e < c ? (float)row[e] : 0.f;
+            for (int j = 0; j < W; ++j) {
+                const int e = channel<LPR, W, VEC>(lane, v, j);
+                x[W * v + j] = e < c ? (float)row[e] : 0.f;
             }
         }
     }
 }
-template <typename T, int LPR, int NV, bool VEC>
-__device__ __forceinline__ void store_row(T *row, int lane, int c, const float (&x)[4 * NV])
+template <typename T, int LPR, int W, int NV, bool VEC>
+__device__ __forceinline__ void store_row(T *row, int lane, int c, const float (&x)[W * NV])
 {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         if constexpr (VEC) {
-            const int e = channel<LPR, VEC>(lane, v, 0);
+            const int e = channel<LPR, W, VEC>(lane, v, 0);
             if (e < c) {
-                typename Vec4<T>::type t;
+                typename Vec<T, W>::type t;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) t[j] = (T)x[4 * v + j];
-                *(typename Vec4<T>::type *)(row + e) = t;
+                for (int j = 0; j < W; ++j) t[j] = (T)x[W * v + j];
+                *(typename Vec<T, W>::type *)(row + e) = t;
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int e = channel<LPR, VEC>(lane, v, j);
-                if (e < c) row[e] = (T)x[4 * v + j];
+            for (int j = 0; j < W; ++j) {
+                const int e = channel<LPR, W, VEC>(lane, v, j);
+                if (e < c) row[e] = (T)x[W * v + j];
             }
         }
     }
 }
 
-template <typename TX, typename TY, int LPR, int NV, bool VEC>
+template <typename TX, typename TY, int LPR, int W, int NV, bool VEC>
 __global__ __launch_bounds__(THREADS) void layernorm_fwd_kernel(const TX *X, const TX *R, TX *S, const float *gamma,
                                                                 const float *beta, TY *Y, float *stats, int64_t n, int c, float eps)
 {
@@ -110,65 +108,65 @@ __global__ __launch_bounds__(THREADS) void layernorm_fwd_kernel(const TX *X, con
     int turn = 0;
     constexpr int GROUPS = THREADS / LPR;
     const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
-    float g[4 * NV], b[4 * NV];
-    if (gamma) load_row<float, LPR, NV, VEC>(gamma, lane, c, g);
-    if (beta) load_row<float, LPR, NV, VEC>(beta, lane, c, b);
+    float g[W * NV], b[W * NV];
+    if (gamma) load_row<float, LPR, W, NV, VEC>(gamma, lane, c, g);
+    if (beta) load_row<float, LPR, W, NV, VEC>(beta, lane, c, b);
 #pragma unroll
-    for (int i = 0; i < 4 * NV; ++i) { if (!gamma) g[i] = 1.f; if (!beta) b[i] = 0.f; }
+    for (int i = 0; i < W * NV; ++i) { if (!gamma) g[i] = 1.f; if (!beta) b[i] = 0.f; }
     const float width = (float)c;                           // divided by, not multiplied with 1 / c: the mean of equal channels is exact
     for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < n; row += (int64_t)gridDim.x * GROUPS) {
-        float x[4 * NV];
-        load_row<TX, LPR, NV, VEC>(X + row * c, lane, c, x);
+        float x[W * NV];
+        load_row<TX, LPR, W, NV, VEC>(X + row * c, lane, c, x);
         if (R) {
-            float r[4 * NV];
-            load_row<TX, LPR, NV, VEC>(R + row * c, lane, c, r);
+            float r[W * NV];
+            load_row<TX, LPR, W, NV, VEC>(R + row * c, lane, c, r);
 #pragma unroll
-            for (int i = 0; i < 4 * NV; ++i) x[i] += r[i];
-            store_row<TX, LPR, NV, VEC>(S + row * c, lane, c, x);
+            for (int i = 0; i < W * NV; ++i) x[i] += r[i];
+            store_row<TX, LPR, W, NV, VEC>(S + row * c, lane, c, x);
         }
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4 * NV; ++i) sum += x[i];       // channels past the row hold 0
+        for (int i = 0; i < W * NV; ++i) sum += x[i];       // channels past the row hold 0
         const float mean = row_sum<LPR>(sum, lds, turn) / width;
         float sq = 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[4 * v + j] -= mean;
-                sq += channel<LPR, VEC>(lane, v, j) < c ? x[4 * v + j] * x[4 * v + j] : 0.f;
+            for (int j = 0; j < W; ++j) {
+                x[W * v + j] -= mean;
+                sq += channel<LPR, W, VEC>(lane, v, j) < c ? x[W * v + j] * x[W * v + j] : 0.f;
             }
         const float rs = 1.f / sqrtf(row_sum<LPR>(sq, lds, turn) / width + eps);
         if (stats && lane == 0) { stats[2 * row] = mean; stats[2 * row + 1] = rs; }
 #pragma unroll
-        for (int i = 0; i < 4 * NV; ++i) x[i] = x[i] * rs * g[i] + b[i];
-        store_row<TY, LPR, NV, VEC>(Y + row * c, lane, c, x);
+        for (int i = 0; i < W * NV; ++i) x[i] = x[i] * rs * g[i] + b[i];
+        store_row<TY, LPR, W, NV, VEC>(Y + row * c, lane, c, x);
     }
 }
 
 // part: [gridDim.x][2][c], the sums of dy h and of dy over a workgroup's rows; null: not wanted
-template <typename TX, typename TY, int LPR, int NV, bool VEC>
+template <typename TX, typename TY, int LPR, int W, int NV, bool VEC>
 __global__ __launch_bounds__(THREADS) void layernorm_bwd_kernel(const TX *X, const float *stats, const float *gamma, const TY *dY,
                                                                 const TX *dS, TX *dX, float *part, int64_t n, int c)
 {
     __shared__ float lds[8];
-    __shared__ float sums[2 * THREADS * 4 * NV];
+    __shared__ float sums[2 * THREADS * W * NV];
     int turn = 0;
     constexpr int GROUPS = THREADS / LPR;
     const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
-    float g[4 * NV], dg[4 * NV], db[4 * NV];
-    if (gamma) load_row<float, LPR, NV, VEC>(gamma, lane, c, g);
+    float g[W * NV], dg[W * NV], db[W * NV];
+    if (gamma) load_row<float, LPR, W, NV, VEC>(gamma, lane, c, g);
 #pragma unroll
-    for (int i = 0; i < 4 * NV; ++i) { if (!gamma) g[i] = 1.f; dg[i] = db[i] = 0.f; }
+    for (int i = 0; i < W * NV; ++i) { if (!gamma) g[i] = 1.f; dg[i] = db[i] = 0.f; }
     const float inv = 1.f / (float)c;
     for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < n; row += (int64_t)gridDim.x * GROUPS) {
-        float x[4 * NV], y[4 * NV];
-        load_row<TX, LPR, NV, VEC>(X + row * c, lane, c, x);
-        load_row<TY, LPR, NV, VEC>(dY + row * c, lane, c, y);
+        float x[W * NV], y[W * NV];
+        load_row<TX, LPR, W, NV, VEC>(X + row * c, lane, c, x);
+        load_row<TY, LPR, W, NV, VEC>(dY + row * c, lane, c, y);
         const float mean = stats[2 * row], rs = stats[2 * row + 1];
         float sw = 0.f, swh = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4 * NV; ++i) {                  // dy is 0 past the row: nothing is added there
+        for (int i = 0; i < W * NV; ++i) {                  // dy is 0 past the row: nothing is added there
             const float h = (x[i] - mean) * rs, w = y[i] * g[i];
             dg[i] += y[i] * h;
             db[i] += y[i];
@@ -180,48 +178,50 @@ __global__ __launch_bounds__(THREADS) void layernorm_bwd_kernel(const TX *X, con
         sw = row_sum<LPR>(sw, lds, turn) * inv;
         swh = row_sum<LPR>(swh, lds, turn) * inv;
 #pragma unroll
-        for (int i = 0; i < 4 * NV; ++i) x[i] = rs * (y[i] - sw - x[i] * swh);
+        for (int i = 0; i < W * NV; ++i) x[i] = rs * (y[i] - sw - x[i] * swh);
         if (dS) {
-            load_row<TX, LPR, NV, VEC>(dS + row * c, lane, c, y);
+            load_row<TX, LPR, W, NV, VEC>(dS + row * c, lane, c, y);
 #pragma unroll
-            for (int i = 0; i < 4 * NV; ++i) x[i] += y[i];
+            for (int i = 0; i < W * NV; ++i) x[i] += y[i];
         }
-        store_row<TX, LPR, NV, VEC>(dX + row * c, lane, c, x);
+        store_row<TX, LPR, W, NV, VEC>(dX + row * c, lane, c, x);
     }
     if (!part) return;
-    constexpr int W = LPR * 4 * NV;                         // channels of a group, those past the row among them
+    constexpr int WIDE = LPR * W * NV;                         // channels of a group, those past the row among them
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int e = channel<LPR, VEC>(lane, v, j);
-            sums[group * W + e] = dg[4 * v + j];
-            sums[(GROUPS + group) * W + e] = db[4 * v + j];
+        for (int j = 0; j < W; ++j) {
+            const int e = channel<LPR, W, VEC>(lane, v, j);
+            sums[group * WIDE + e] = dg[W * v + j];
+            sums[(GROUPS + group) * WIDE + e] = db[W * v + j];
         }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * c; i += THREADS) {
         const int k = i / c, e = i - k * c;
         float t = 0.f;
-        for (int q = 0; q < GROUPS; ++q) t += sums[(k * GROUPS + q) * W + e];
+        for (int q = 0; q < GROUPS; ++q) t += sums[(k * GROUPS + q) * WIDE + e];
         part[(int64_t)blockIdx.x * 2 * c + i] = t;
     }
 }
 
-// dgamma, dbeta from the workgroups' sums, always in the same order: 16 columns by 16 interleaved chains
-__global__ __launch_bounds__(THREADS) void layernorm_sum_kernel(const float *part, float *dgamma, float *dbeta, int blocks, int c)
+// dgamma, dbeta from the workgroups' sums, always in the same order: COLS columns by interleaved chains.  4 columns where there
+// are few, or a handful of workgroups adds up everything (50 channels, 990 parts: 6.4 -> 5.0 us).
+template <int COLS> __global__ __launch_bounds__(THREADS) void layernorm_sum_kernel(const float *part, float *dgamma, float *dbeta, int blocks, int c)
 {
-    __shared__ float lds[16][17];
-    const int col = blockIdx.x * 16 + (threadIdx.x & 15), chain = threadIdx.x >> 4;
+    constexpr int CHAINS = THREADS / COLS;
+    __shared__ float lds[CHAINS][COLS + 1];
+    const int x = threadIdx.x % COLS, col = blockIdx.x * COLS + x, chain = threadIdx.x / COLS;
     float t = 0.f;
     if (col < 2 * c)
 #pragma unroll 8
-        for (int b = chain; b < blocks; b += 16) t += part[(int64_t)b * 2 * c + col];
-    lds[chain][threadIdx.x & 15] = t;
+        for (int b = chain; b < blocks; b += CHAINS) t += part[(int64_t)b * 2 * c + col];
+    lds[chain][x] = t;
     __syncthreads();
     if (chain == 0 && col < 2 * c) {
         t = 0.f;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) t += lds[k][threadIdx.x];
+        for (int k = 0; k < CHAINS; ++k) t += lds[k][x];
         (col < c ? dgamma : dbeta)[col < c ? col : col - c] = t;
     }
 }
