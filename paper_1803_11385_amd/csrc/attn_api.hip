@@ -49,9 +49,12 @@ Plan plan(const hch_attn_desc &p, int64_t rows, int heads, double stream, double
             if (splits < 1 || splits > steps || (splits > 1 && wgs * splits > 4 * UNITS)) continue;
             const double each = std::ceil(wgs * splits / UNITS), busy = each <= 1.0 ? 1.0 : std::max(1.0, each / st.at_once);
             double us = (START + std::ceil(UNEVEN * steps / splits) * st.us * cost) * busy;
-            // Memory: at its rate if the compute units share evenly, and not with more than two workgroups each at it (8 shapes
-            // of 76165 keys, 2 heads of 32, bf16: 512 workgroups 26 us, 768 33, 1024 42).
-            us = std::max(us, moved / MEMORY * each * UNITS / (wgs * splits) * (each > 2.0 ? 1.2 : 1.0));
+            // Memory: at its rate if the compute units share evenly.  Shapes of different lengths do not split into equal parts, which
+            // several workgroups a unit even out (one query for each of 8 shapes of 609323 keys together, 2 heads of 32, bf16: 256 workgroups 70 us,
+            // 512 42, 768 36, 1024 47; 304000 keys, 4 heads of 64: 93, 70, 65, 66).
+            const double share = p.batch == 1 ? (each > 2.0 ? 1.1 : 1.0) : each <= 1.0 ? 1.45 : each <= 2.0 ? 1.12 : each <= 3.0 ? 1.0 : 1.1;
+            const double move = moved / MEMORY * each * UNITS / (wgs * splits) * share;
+            us = std::max(us, move) + 0.2 * std::min(us, move);         // (they do not overlap altogether)
             if (splits > 1) us += JOIN + JOIN_SPLIT * splits + 2.0 * splits * rows * heads * width / BYTES_PER_US;
             if (best.slots == 0 || us < least) {
                 least = us;
