@@ -502,8 +502,9 @@ hch_status hch_relu_bwd(const float *y, const float *dy, float *dx, int64_t n, v
  * An attention block over the voxels of a level: layer norm, rotary positions, attention inside each
  * shape.  Rows are voxels, voxel-major as everywhere; the linear layers between them are convolutions with
  * F = 1 (hch_sconv_*).  16-bit tensors are bfloat16 bit patterns; sums, statistics and softmax are kept in fp32
- * and rounded once, when an output is stored.  Every call is asynchronous on `stream`, allocates nothing and
- * gives the same bits in every run.  Nothing is written on error.
+ * and rounded once, when an output is stored.  Every call is asynchronous on `stream`, allocates nothing on the device
+ * and gives the same bits in every run.  Nothing is written on error (HCH_ENOMEM: host memory for a message or a
+ * kernel's first launch).  A workspace belongs to one call at a time: calls that may overlap need one each.
  * --------------------------------------------------------------------------------------------- */
 
 /*

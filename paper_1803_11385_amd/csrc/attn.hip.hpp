@@ -100,6 +100,7 @@ __device__ __forceinline__ f32x16 mfma16(bf16x8 a, bf16x8 b, f32x16 c) { return 
 
 struct Bf16 {
     typedef __bf16 T;
+    static constexpr const char *NAME = "attn::Bf16";
     static constexpr int PLANES = 1, AHEAD = 4;
     typedef bf16x8 Part;
     static __device__ __forceinline__ Part part(const __bf16 (&x)[8]) { return __builtin_bit_cast(bf16x8, x); }
@@ -123,6 +124,7 @@ struct Bf16 {
 // are lost one by one as they fall below 2^-133; an infinite operand makes its sums NaN.)
 struct Split {
     typedef float T;
+    static constexpr const char *NAME = "attn::Split";
     static constexpr int PLANES = 3, AHEAD = 1;
     struct Part { bf16x8 v[3]; };
     static __device__ __forceinline__ uint32_t round2(float a, float b)

@@ -1,6 +1,8 @@
 // C entries of attention inside the shapes of a ragged batch.
 #include <algorithm>
 #include <cmath>
+#include <exception>
+#include <initializer_list>
 
 #include "attn_launch.hpp"
 
@@ -154,15 +156,17 @@ double pairs(const hch_attn_desc &p) { return (double)p.n_q * p.n_k / std::max(1
 }  // namespace
 
 extern "C" size_t hch_attn_workspace_bytes(const hch_attn_desc *desc, hch_ws_kind kind)
-{
+try {
     if (check_sizes("hch_attn_workspace_bytes", desc) != HCH_OK || (kind != HCH_WS_FWD && kind != HCH_WS_BWD_DATA)) return 0;
     if (!desc->n_q) return 256;
     return kind == HCH_WS_FWD ? fwd_bytes(*desc, plan_keys(*desc, FWD)) : bwd_bytes(*desc, plan_keys(*desc, DQ), plan_queries(*desc));
+} catch (const std::exception &) {
+    return 0;
 }
 
 extern "C" hch_status hch_attn_fwd(const hch_attn_desc *desc, const void *Q, const void *K, const void *V, void *O, float *lse,
                                    void *workspace, size_t ws_bytes, void *stream)
-{
+try {
     hch_status st = check_sizes("hch_attn_fwd", desc);
     if (st != HCH_OK) return st;
     const hch_attn_desc &p = *desc;
@@ -181,11 +185,13 @@ extern "C" hch_status hch_attn_fwd(const hch_attn_desc *desc, const void *Q, con
     const double bytes = row_bytes(p, 2, 2), flops = 4 * pairs(p);
     return p.dtype == HCH_F32 ? hch::attn::launch_fwd<float>(a, r.narrow, bytes, flops, (hipStream_t)stream)
                               : hch::attn::launch_fwd<__bf16>(a, r.narrow, bytes, flops, (hipStream_t)stream);
+} catch (const std::exception &) {
+    return HCH_ENOMEM;
 }
 
 extern "C" hch_status hch_attn_bwd(const hch_attn_desc *desc, const void *Q, const void *K, const void *V, const void *O, const float *lse,
                                    const void *dO, void *dQ, void *dK, void *dV, void *workspace, size_t ws_bytes, void *stream)
-{
+try {
     hch_status st = check_sizes("hch_attn_bwd", desc);
     if (st != HCH_OK) return st;
     const hch_attn_desc &p = *desc;
@@ -218,4 +224,6 @@ extern "C" hch_status hch_attn_bwd(const hch_attn_desc *desc, const void *Q, con
                                 : hch::attn::launch_bwd_dkv<__bf16>(a, rk.narrow, bytes, flops, s);
     }
     return st;
+} catch (const std::exception &) {
+    return HCH_ENOMEM;
 }

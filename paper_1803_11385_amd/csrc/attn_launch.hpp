@@ -1,6 +1,8 @@
 // Launches of the attention kernels: the choice of an instance by element type and head width.  The instances of a type
 // are compiled in a source of their own (attn_bf16.hip, attn_f32.hip).
 #pragma once
+#include <cstdio>
+
 #include "api_common.hpp"
 #include "attn.hip.hpp"
 
@@ -28,30 +30,48 @@ template <typename T, typename F> void with_width(int d, bool narrow, bool vec, 
     else if (d <= 96 && !(narrow && sizeof(T) == 4)) g(std::integral_constant<int, 96>{});
     else g(std::integral_constant<int, 128>{});
 }
+// id of an instance's name, as a profiler prints it
+inline int instance_id(const char *kernel, const char *engine, int d, int form, bool vec)
+{
+    char name[96];
+    snprintf(name, sizeof name, "%s<%s, %d, %d, %s>", kernel, engine, d, form, vec ? "true" : "false");
+    return Profiler::get().id_for(name);
+}
+template <typename T> constexpr const char *TYPE_NAME = sizeof(T) == 4 ? "float" : "__bf16";
+inline int join_id(const char *kernel, const char *type, int groups)
+{
+    char name[64];
+    if (groups) snprintf(name, sizeof name, "%s<%s, %d>", kernel, type, groups);
+    else snprintf(name, sizeof name, "%s<%s>", kernel, type);
+    return Profiler::get().id_for(name);
+}
+
 template <typename T, int D> constexpr bool has_narrow = sizeof(T) == 2 || D != 96;
 
 template <typename T> hch_status launch_fwd(const Args &a, bool narrow, double bytes, double flops, hipStream_t s)
 {
-    {
-        LaunchTimer lt(HCH_KERNEL_ID("attn_fwd_kernel"), s, bytes, flops);
-        with_width<T>(a.d, narrow, a.vec, [&](auto w, auto v) {
-            typedef typename EngineOf<T>::E E;
-            constexpr int D = decltype(w)::value;
-            constexpr bool V = decltype(v)::value;
-            if (!narrow) {
-                constexpr auto kernel = attn_fwd_kernel<E, D, 4, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
-            } else if constexpr (has_narrow<T, D>) {
-                constexpr auto kernel = attn_fwd_kernel<E, D, 1, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
-            }
-        });
-    }
+    with_width<T>(a.d, narrow, a.vec, [&](auto w, auto v) {
+        typedef typename EngineOf<T>::E E;
+        constexpr int D = decltype(w)::value;
+        constexpr bool V = decltype(v)::value;
+        if (!narrow) {
+            static const int id = instance_id("attn::attn_fwd_kernel", E::NAME, D, 4, V);
+            constexpr auto kernel = attn_fwd_kernel<E, D, 4, V>;
+            LaunchTimer lt(id, s, bytes, flops);
+            HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
+        } else if constexpr (has_narrow<T, D>) {
+            static const int id = instance_id("attn::attn_fwd_kernel", E::NAME, D, 1, V);
+            constexpr auto kernel = attn_fwd_kernel<E, D, 1, V>;
+            LaunchTimer lt(id, s, bytes, flops);
+            HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
+        }
+    });
     HCH_LAUNCH_CHECK("attn_fwd_kernel");
     if (a.splits > 1) {
         {
-            LaunchTimer lt(HCH_KERNEL_ID("attn_join_kernel"), s, (double)a.splits * a.nq * a.hq * (4 * a.d + 8), 0.0);
             const int64_t rows = a.nq * a.hq;
+            static const int id1 = join_id("attn::attn_join_kernel", TYPE_NAME<T>, 1), id8 = join_id("attn::attn_join_kernel", TYPE_NAME<T>, 8);
+            LaunchTimer lt(a.splits <= 8 || rows >= 4096 ? id1 : id8, s, (double)a.splits * rows * (4 * a.d + 8), 0.0);
             constexpr auto one = attn_join_kernel<T, 1>;
             constexpr auto eight = attn_join_kernel<T, 8>;
             if (a.splits <= 8 || rows >= 4096) HCH_LAUNCH(one, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, a);
@@ -64,25 +84,27 @@ template <typename T> hch_status launch_fwd(const Args &a, bool narrow, double b
 
 template <typename T> hch_status launch_bwd_dq(const Args &a, bool narrow, double bytes, double flops, hipStream_t s)
 {
-    {
-        LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_dq_kernel"), s, bytes, flops);
-        with_width<T>(a.d, narrow, a.vec, [&](auto w, auto v) {
-            typedef typename EngineOf<T>::E E;
-            constexpr int D = decltype(w)::value;
-            constexpr bool V = decltype(v)::value;
-            if (!narrow) {
-                constexpr auto kernel = attn_bwd_dq_kernel<E, D, 4, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
-            } else if constexpr (has_narrow<T, D>) {
-                constexpr auto kernel = attn_bwd_dq_kernel<E, D, 1, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
-            }
-        });
-    }
+    with_width<T>(a.d, narrow, a.vec, [&](auto w, auto v) {
+        typedef typename EngineOf<T>::E E;
+        constexpr int D = decltype(w)::value;
+        constexpr bool V = decltype(v)::value;
+        if (!narrow) {
+            static const int id = instance_id("attn::attn_bwd_dq_kernel", E::NAME, D, 4, V);
+            constexpr auto kernel = attn_bwd_dq_kernel<E, D, 4, V>;
+            LaunchTimer lt(id, s, bytes, flops);
+            HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 4, V>::THREADS)), 0, s, a);
+        } else if constexpr (has_narrow<T, D>) {
+            static const int id = instance_id("attn::attn_bwd_dq_kernel", E::NAME, D, 1, V);
+            constexpr auto kernel = attn_bwd_dq_kernel<E, D, 1, V>;
+            LaunchTimer lt(id, s, bytes, flops);
+            HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Keys<E, D, 1, V>::THREADS)), 0, s, a);
+        }
+    });
     HCH_LAUNCH_CHECK("attn_bwd_dq_kernel");
     if (a.splits > 1) {
         {
-            LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_join_kernel"), s, (double)a.splits * a.nq * a.hq * 4 * a.d, 0.0);
+            static const int id = join_id("attn::attn_bwd_join_kernel", TYPE_NAME<T>, 0);
+            LaunchTimer lt(id, s, (double)a.splits * a.nq * a.hq * 4 * a.d, 0.0);
             constexpr auto kernel = attn_bwd_join_kernel<T>;
             HCH_LAUNCH(kernel, dim3((unsigned)((a.nq * a.hq * a.d + 255) / 256)), dim3(256), 0, s, a);
         }
@@ -93,25 +115,27 @@ template <typename T> hch_status launch_bwd_dq(const Args &a, bool narrow, doubl
 
 template <typename T> hch_status launch_bwd_dkv(const Args &a, bool narrow, double bytes, double flops, hipStream_t s)
 {
-    {
-        LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_dkv_kernel"), s, bytes, flops);
-        with_width<T>(a.d, narrow, a.vec, [&](auto w, auto v) {
-            typedef typename EngineOf<T>::E E;
-            constexpr int D = decltype(w)::value;
-            constexpr bool V = decltype(v)::value;
-            if (!narrow) {
-                constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 4, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Queries<E, D, 4, V>::THREADS)), 0, s, a);
-            } else if constexpr (has_narrow<T, D>) {
-                constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 1, V>;
-                HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Queries<E, D, 1, V>::THREADS)), 0, s, a);
-            }
-        });
-    }
+    with_width<T>(a.d, narrow, a.vec, [&](auto w, auto v) {
+        typedef typename EngineOf<T>::E E;
+        constexpr int D = decltype(w)::value;
+        constexpr bool V = decltype(v)::value;
+        if (!narrow) {
+            static const int id = instance_id("attn::attn_bwd_dkv_kernel", E::NAME, D, 4, V);
+            constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 4, V>;
+            LaunchTimer lt(id, s, bytes, flops);
+            HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Queries<E, D, 4, V>::THREADS)), 0, s, a);
+        } else if constexpr (has_narrow<T, D>) {
+            static const int id = instance_id("attn::attn_bwd_dkv_kernel", E::NAME, D, 1, V);
+            constexpr auto kernel = attn_bwd_dkv_kernel<E, D, 1, V>;
+            LaunchTimer lt(id, s, bytes, flops);
+            HCH_LAUNCH(kernel, dim3(work_grid(a)), dim3((Queries<E, D, 1, V>::THREADS)), 0, s, a);
+        }
+    });
     HCH_LAUNCH_CHECK("attn_bwd_dkv_kernel");
     if (a.splits > 1) {
         {
-            LaunchTimer lt(HCH_KERNEL_ID("attn_bwd_join_keys_kernel"), s, (double)a.splits * a.nk * a.hkv * 8 * a.d, 0.0);
+            static const int id = join_id("attn::attn_bwd_join_keys_kernel", TYPE_NAME<T>, 0);
+            LaunchTimer lt(id, s, (double)a.splits * a.nk * a.hkv * 8 * a.d, 0.0);
             constexpr auto kernel = attn_bwd_join_keys_kernel<T>;
             HCH_LAUNCH(kernel, dim3((unsigned)((2 * a.nk * a.hkv * a.d + 255) / 256)), dim3(256), 0, s, a);
         }

@@ -3,6 +3,9 @@
 
 #include <algorithm>
 #include <cmath>
+#include <exception>
+#include <initializer_list>
+#include <type_traits>
 
 #include "norm.hip.hpp"
 #include "rope.hip.hpp"
@@ -46,6 +49,14 @@ template <typename F> void with_row_shape(int c, bool wide, bool vec, F &&f)
 #undef HCH_SHAPE
 }
 
+// id of an instance's name, as a profiler prints it: types, then numbers, then a truth value
+template <typename TX, typename TY> int instance_id(const char *kernel, std::initializer_list<int> numbers, bool vec)
+{
+    std::string name = std::string(kernel) + "<" + (sizeof(TX) == 4 ? "float" : "__bf16") + ", " + (sizeof(TY) == 4 ? "float" : "__bf16");
+    for (int i : numbers) name += ", " + std::to_string(i);
+    return hch::Profiler::get().id_for(name + (vec ? ", true>" : ", false>"));
+}
+
 template <typename F> void with_types(hch_dtype a, hch_dtype b, F &&f)
 {
     if (a == HCH_F32 && b == HCH_F32) f(float{}, float{});
@@ -58,7 +69,7 @@ template <typename F> void with_types(hch_dtype a, hch_dtype b, F &&f)
 
 extern "C" hch_status hch_layernorm_fwd(hch_dtype x_dtype, const void *X, const void *R, void *S, const float *gamma, const float *beta,
                                         hch_dtype y_dtype, void *Y, float *stats, int64_t n, int32_t c, float eps, void *stream)
-{
+try {
     if (!known(x_dtype) || !known(y_dtype)) return fail(HCH_EINVAL, "hch_layernorm_fwd: unknown dtype");
     if (!X || !Y || (R != nullptr) != (S != nullptr)) return fail(HCH_EINVAL, "hch_layernorm_fwd: null pointer, or only one of R and S");
     if (n < 0 || c <= 0 || !(eps >= 0.f)) return fail(HCH_EINVAL, "hch_layernorm_fwd: bad size or eps");
@@ -71,12 +82,12 @@ extern "C" hch_status hch_layernorm_fwd(hch_dtype x_dtype, const void *X, const 
     const int groups = hch::norm::THREADS / row_shape(c, wide ? 8 : 4).lpr;
     const unsigned grid = (unsigned)std::min<int64_t>((n + groups - 1) / groups, 4096);
     {
-        hch::LaunchTimer lt(HCH_KERNEL_ID("layernorm_fwd_kernel"), (hipStream_t)stream,
-                            (double)n * c * (size_of(x_dtype) * (R ? 3 : 1) + size_of(y_dtype)), 8.0 * n * c);
         with_types(x_dtype, y_dtype, [&](auto tx, auto ty) {
             using TX = decltype(tx);
             using TY = decltype(ty);
             with_row_shape(c, wide, vec, [&](auto l, auto w, auto v, auto b) {
+                static const int id = instance_id<TX, TY>("norm::layernorm_fwd_kernel", {decltype(l)::value, decltype(w)::value, decltype(v)::value}, decltype(b)::value);
+                hch::LaunchTimer lt(id, (hipStream_t)stream, (double)n * c * (size_of(x_dtype) * (R ? 3 : 1) + size_of(y_dtype)), 8.0 * n * c);
                 constexpr auto kernel = hch::norm::layernorm_fwd_kernel<TX, TY, decltype(l)::value, decltype(w)::value, decltype(v)::value, decltype(b)::value>;
                 HCH_LAUNCH(kernel, dim3(grid), dim3(hch::norm::THREADS), 0, (hipStream_t)stream, (const TX *)X, (const TX *)R, (TX *)S,
                            gamma, beta, (TY *)Y, stats, n, c, eps);
@@ -85,6 +96,8 @@ extern "C" hch_status hch_layernorm_fwd(hch_dtype x_dtype, const void *X, const 
     }
     HCH_LAUNCH_CHECK("layernorm_fwd_kernel");
     return HCH_OK;
+} catch (const std::exception &) {
+    return HCH_ENOMEM;
 }
 
 extern "C" size_t hch_layernorm_workspace_bytes(int64_t n, int32_t c)
@@ -96,7 +109,7 @@ extern "C" size_t hch_layernorm_workspace_bytes(int64_t n, int32_t c)
 extern "C" hch_status hch_layernorm_bwd(hch_dtype x_dtype, const void *X, const float *stats, const float *gamma, hch_dtype dy_dtype,
                                         const void *dY, const void *dS, void *dX, float *dgamma, float *dbeta, int64_t n, int32_t c,
                                         void *workspace, size_t ws_bytes, void *stream)
-{
+try {
     if (!known(x_dtype) || !known(dy_dtype)) return fail(HCH_EINVAL, "hch_layernorm_bwd: unknown dtype");
     if (!X || !stats || !dY || !dX || (dgamma != nullptr) != (dbeta != nullptr))
         return fail(HCH_EINVAL, "hch_layernorm_bwd: null pointer, or only one of dgamma and dbeta");
@@ -115,12 +128,12 @@ extern "C" hch_status hch_layernorm_bwd(hch_dtype x_dtype, const void *X, const 
         const bool wide = vec && x_dtype == HCH_BF16 && c % 8 == 0 && c <= 1024 && aligned(X, 16) && aligned(dS, 16) && aligned(dX, 16) &&
                           aligned(dY, 16);
         {
-            hch::LaunchTimer lt(HCH_KERNEL_ID("layernorm_bwd_kernel"), (hipStream_t)stream,
-                                (double)n * c * (size_of(x_dtype) * (dS ? 3 : 2) + size_of(dy_dtype)) + 8.0 * n, 14.0 * n * c);
             with_types(x_dtype, dy_dtype, [&](auto tx, auto ty) {
                 using TX = decltype(tx);
                 using TY = decltype(ty);
                 with_row_shape(c, wide, vec, [&](auto l, auto w, auto v, auto b) {
+                    static const int id = instance_id<TX, TY>("norm::layernorm_bwd_kernel", {decltype(l)::value, decltype(w)::value, decltype(v)::value}, decltype(b)::value);
+                    hch::LaunchTimer lt(id, (hipStream_t)stream, (double)n * c * (size_of(x_dtype) * (dS ? 3 : 2) + size_of(dy_dtype)) + 8.0 * n, 14.0 * n * c);
                     constexpr auto kernel = hch::norm::layernorm_bwd_kernel<TX, TY, decltype(l)::value, decltype(w)::value, decltype(v)::value, decltype(b)::value>;
                     HCH_LAUNCH(kernel, dim3(blocks), dim3(hch::norm::THREADS), 0, (hipStream_t)stream, (const TX *)X, stats, gamma,
                                (const TY *)dY, (const TX *)dS, (TX *)dX, part, n, c);
@@ -131,7 +144,7 @@ extern "C" hch_status hch_layernorm_bwd(hch_dtype x_dtype, const void *X, const 
     }
     if (dgamma) {
         {
-            hch::LaunchTimer lt(HCH_KERNEL_ID("layernorm_sum_kernel"), (hipStream_t)stream, 8.0 * blocks * c, 2.0 * blocks * c);
+            hch::LaunchTimer lt(2 * c <= 256 ? HCH_KERNEL_ID("norm::layernorm_sum_kernel<4>") : HCH_KERNEL_ID("norm::layernorm_sum_kernel<16>"), (hipStream_t)stream, 8.0 * blocks * c, 2.0 * blocks * c);
             if (2 * c <= 256)
                 HCH_LAUNCH(hch::norm::layernorm_sum_kernel<4>, dim3((2 * c + 3) / 4), dim3(hch::norm::THREADS), 0, (hipStream_t)stream, part, dgamma,
                            dbeta, blocks, c);
@@ -142,6 +155,8 @@ extern "C" hch_status hch_layernorm_bwd(hch_dtype x_dtype, const void *X, const 
         HCH_LAUNCH_CHECK("layernorm_sum_kernel");
     }
     return HCH_OK;
+} catch (const std::exception &) {
+    return HCH_ENOMEM;
 }
 
 namespace {
@@ -181,12 +196,12 @@ hch_status rope(const char *who, double sign, hch_dtype x_dtype, const void *X, 
     const int64_t blocks = (n + rows - 1) / rows;
     if (blocks > 0x7fffffff || (int64_t)heads * head_dim > (1 << 22)) return fail(HCH_EUNSUPPORTED, name + ": too many rows or heads for one launch");
     {
-        hch::LaunchTimer lt(HCH_KERNEL_ID("rope_kernel"), (hipStream_t)stream, (double)n * heads * head_dim * (sx + sy) + 12.0 * n,
-                            6.0 * n * rot_heads * pairs);
         with_types(x_dtype, y_dtype, [&](auto tx, auto ty) {
             using TX = decltype(tx);
             using TY = decltype(ty);
             auto launch = [&](auto k, auto v) {
+                static const int id = instance_id<TX, TY>("rope::rope_kernel", {decltype(k)::value}, decltype(v)::value);
+                hch::LaunchTimer lt(id, (hipStream_t)stream, (double)n * heads * head_dim * (sx + sy) + 12.0 * n, 6.0 * n * rot_heads * pairs);
                 constexpr auto kernel = hch::rope::rope_kernel<TX, TY, decltype(k)::value, decltype(v)::value>;
                 HCH_LAUNCH(kernel, dim3((unsigned)blocks, (unsigned)((pieces + hch::rope::THREADS - 1) / hch::rope::THREADS)), dim3(hch::rope::THREADS),
                            0, (hipStream_t)stream, (const TX *)X, ld_x, (TY *)Y, ld_y, coords, n, pieces, wide, rows, rot_heads, head_dim, turned, table);
@@ -205,13 +220,17 @@ hch_status rope(const char *who, double sign, hch_dtype x_dtype, const void *X, 
 extern "C" hch_status hch_rope_fwd(hch_dtype x_dtype, const void *X, int64_t ld_x, hch_dtype y_dtype, void *Y, int64_t ld_y,
                                    const int32_t *coords, int64_t n, int32_t heads, int32_t rot_heads, int32_t head_dim,
                                    const int32_t *sections, float base, float scale, void *stream)
-{
+try {
     return rope("hch_rope_fwd", 1.0, x_dtype, X, ld_x, y_dtype, Y, ld_y, coords, n, heads, rot_heads, head_dim, sections, base, scale, stream);
+} catch (const std::exception &) {
+    return HCH_ENOMEM;
 }
 
 extern "C" hch_status hch_rope_bwd(hch_dtype dy_dtype, const void *dY, int64_t ld_dy, hch_dtype dx_dtype, void *dX, int64_t ld_dx,
                                    const int32_t *coords, int64_t n, int32_t heads, int32_t rot_heads, int32_t head_dim,
                                    const int32_t *sections, float base, float scale, void *stream)
-{
+try {
     return rope("hch_rope_bwd", -1.0, dy_dtype, dY, ld_dy, dx_dtype, dX, ld_dx, coords, n, heads, rot_heads, head_dim, sections, base, scale, stream);
+} catch (const std::exception &) {
+    return HCH_ENOMEM;
 }

@@ -131,6 +131,51 @@ def test_ragged_shapes_against_the_oracle(dtype, hq, hkv, d):
     Case(dtype, RAGGED, RAGGED, hq, hkv, d, seed=d).run().check()
 
 
+def _launched(run):
+    """Names of the kernels that `run` launched."""
+    hch.hch_profile_enable(-1, 1)
+    hch.hch_profile_reset()
+    run()
+    torch.cuda.synchronize()
+    names = [hch.hch_kernel_name(i) for i in range(hch.hch_kernel_count()) if hch.hch_profile_read(i)["launches"]]
+    hch.hch_profile_enable(-1, 0)
+    hch.hch_profile_reset()
+    return names
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("d", [24, 64, 96, 128])
+def test_both_forms_of_every_width(dtype, pad, d):
+    """Many shapes take tiles of 128 rows, few queries or keys tiles of 32; with addresses and strides in whole pieces and
+    without."""
+    many, some = [100 + 7 * (i % 13) for i in range(70)], [260 + 9 * (i % 5) for i in range(20)]
+    names = set()
+    for lq, lk, hq, hkv in ((many, many, 4, 2), (some, some, 4, 2), ([1, 2], [1500, 700], 4, 2), ([1300, 40], [20, 3], 4, 2),
+                            ([38], [38], 4, 2), ([61], [61], 1, 1), ([43], [43], 4, 2), ([18], [18], 16, 4), ([71, 71], [113, 113], 16, 8),
+                            ([57] * 3, [57] * 3, 8, 4), ([241, 241], [241, 241], 8, 8)):
+        c = Case(dtype, lq, lk, hq, hkv, d, masked=0.1, pad=pad, junk=True, seed=d + pad)
+        names |= set(_launched(c.run))
+        c.check()
+    engine, whole = {"f32": "Split", "bf16": "Bf16"}[dtype], "false" if pad else "true"
+    narrow = 128 if dtype == "f32" and d > 64 else (d + 31) // 32 * 32
+    for kernel in ("attn_fwd_kernel", "attn_bwd_dq_kernel", "attn_bwd_dkv_kernel"):
+        for width, form in (((d + 31) // 32 * 32, 4), (narrow, 1)):
+            assert f"attn::{kernel}<attn::{engine}, {width}, {form}, {whole}>" in names, (kernel, form, sorted(names))
+
+
+def test_splits_of_every_pass_are_joined():
+    c = Case("f32", [900], [1100], 1, 1, 96, masked=0.1, seed=8)
+    names = _launched(c.run)
+    for part in ("attn_join_kernel<float, ", "attn_bwd_join_kernel<float>", "attn_bwd_join_keys_kernel<float>"):
+        assert any(part in n for n in names), names
+    c.check()
+    c = Case("bf16", [1], [60000], 2, 1, 128, seed=9)
+    names = _launched(c.run)
+    assert any("attn_join_kernel<__bf16, 8>" in n for n in names) and any("attn_bwd_join_kernel<__bf16>" in n for n in names), names
+    c.check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("d", [24, 64, 128])
 def test_masks_and_what_they_leave_out(dtype, d):
