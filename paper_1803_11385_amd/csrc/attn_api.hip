@@ -97,6 +97,8 @@ size_t bwd_bytes(const hch_attn_desc &p, const Plan &dq, const Plan &dkv)
     return delta_bytes(p) + std::max<size_t>({256, part_bytes(p, dq.splits), key_part_bytes(p, dkv.splits)});
 }
 
+constexpr int64_t ROWS = 0x7fffffff - 256;              // the last tile's end is an int too
+
 // what both calls and the size query ask of the sizes
 hch_status check_sizes(const char *who, const hch_attn_desc *p)
 {
@@ -106,7 +108,7 @@ hch_status check_sizes(const char *who, const hch_attn_desc *p)
     if (p->batch < 0 || p->n_q < 0 || p->n_k < 0 || p->heads_q <= 0 || p->heads_kv <= 0 || p->head_dim <= 0 || p->heads_q % p->heads_kv)
         return no(HCH_EINVAL, ": bad size, or heads_q not a multiple of heads_kv");
     if (p->head_dim > 128) return no(HCH_EUNSUPPORTED, ": more than 128 channels per head");
-    if (p->n_k > 0x7fffffff || p->n_q > 0x7fffffff / p->heads_q || p->heads_q > 0x7fff) return no(HCH_EUNSUPPORTED, ": more than 2^31 - 1 rows, or 2^15 - 1 heads");
+    if (p->n_k > ROWS || p->n_q > ROWS / p->heads_q || p->heads_q > 0x7fff) return no(HCH_EUNSUPPORTED, ": 2^31 - 256 rows or more, or 2^15 heads or more");
     if (p->batch == 0 && (p->n_q || p->n_k)) return no(HCH_EINVAL, ": rows without a shape");
     return HCH_OK;
 }

@@ -44,6 +44,14 @@ def test_attention_refuses():
     assert _bwd(n_q=0, n_k=0) == 0 and _bwd(batch=0, n_q=0, n_k=0) == 0
 
 
+def test_attention_refuses_rows_whose_last_tile_would_end_beyond_32_bits():
+    last = 2 ** 31 - 257
+    ask = lambda **kw: hch.load_library().hch_attn_workspace_bytes(C.byref(_desc(**kw)), hch.HCH_WS_FWD)
+    assert ask(n_k=last) and not ask(n_k=last + 1)
+    one = dict(heads_q=1, heads_kv=1)
+    assert ask(n_q=last, **one) and not ask(n_q=last + 1, **one) and not ask(n_q=last // 2 + 1, heads_q=2, heads_kv=1)
+
+
 def test_attention_workspace():
     ask = hch.hch_attn_workspace_bytes
     assert ask(hch.HCH_WS_FWD, hch.HCH_F32, 1, 0, 0, 2, 1, 32) == 256
