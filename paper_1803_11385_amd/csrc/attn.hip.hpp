@@ -519,6 +519,12 @@ template <typename E, int D, int QW, bool VEC> struct Keys {
     static constexpr int BUFFER = 2 * TILE + 4 * BK, BUFFERS = QW == 1 || 2 * BUFFER > 80 * 1024 ? 1 : 2;   // two where two workgroups still share a compute unit
     static constexpr int WORDS = (BK + 63) / 64;
     static constexpr bool DIRECT = VEC && E::PLANES == 1 && QW == 4;   // two buffers, so the loads of the next tile need no registers
+    // Workgroups that share a compute unit, i.e. wavefronts a SIMD, i.e. registers: one more where a few registers decide, which
+    // then wait in scratch (fp32, 8 shapes of 2048, 8 heads: dQ of 64 channels 588 us with 260 registers, 501 with 256; of
+    // 32 333 -> 311; bf16, 16 of 4096, 16 heads of 96, forward 1780 -> 1660).  Where more would have to move it is slower (fp32
+    // dQ of 96 channels 870 -> 1725, forward of 128 763 -> 1033).
+    static constexpr int AT_ONCE_FWD = !DIRECT ? 1 : D == 96 ? 3 : 2;
+    static constexpr int AT_ONCE_DQ = DIRECT ? 2 : E::PLANES == 1 || QW == 1 ? 1 : D == 32 ? 3 : D == 64 ? 2 : 1;
     static constexpr int JOIN = QW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = BUFFERS * BUFFER > JOIN ? BUFFERS * BUFFER : JOIN;
 };
 
@@ -528,7 +534,7 @@ template <typename E, int D, int QW, bool VEC> struct Keys {
 // Query rows of the heads that share a key head are one list, row = token * group + (head within the group), so that
 // a tile of keys serves the whole group.
 template <typename E, int D, int QW, bool VEC>
-__global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::DIRECT ? 2 : 1)) void attn_fwd_kernel(Args a)
+__global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::AT_ONCE_FWD)) void attn_fwd_kernel(Args a)
 {
     typedef Keys<E, D, QW, VEC> S;
     typedef Tile<E, D> L;
@@ -542,12 +548,10 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     const Place place = place_of(a.qo, a.nq, a.ko, a.nk, a.batch, a.sorted, a.group, S::BQ, slot, lane);
     if (place.tile < 0) return;
     const Span q = place.own, k = place.stream;
-    const int64_t rows = (int64_t)(q.end - q.begin) * a.group, row0 = (int64_t)place.tile * S::BQ;
-
-    const int64_t row = row0 + 32 * qw + (lane & 31);
+    // n_q * heads_q and a tile more are below 2^31
+    const int rows = (q.end - q.begin) * a.group, row = place.tile * S::BQ + 32 * qw + (lane & 31);
     const bool valid = row < rows;
-    const int64_t token = valid ? q.begin + row / a.group : q.begin;
-    const int head = kvh * a.group + (valid ? (int)(row % a.group) : 0);
+    const int token = q.begin + (valid ? row / a.group : 0), head = kvh * a.group + (valid ? row % a.group : 0), at = token * a.hq + head;
     const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
     const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
@@ -694,13 +698,12 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
             }
     }
     if (!valid) return;
-    const int64_t at = token * a.hq + head;
     const int e0 = 32 * S::DT * dw;
     if (a.splits == 1) {
         store_row<T>((T *)a.Ow + token * a.ld_o + (int64_t)head * a.d + e0, acc, l > 0.f || l != l ? 1.f / l : 0.f, a.d - e0, VEC, h);
         if (a.lse && h == 0 && dw == 0) a.lse[at] = l > 0.f || l != l ? m * LN2 + logf(l) : -INFINITY;
     } else {
-        const int64_t p = (int64_t)split * a.nq * a.hq + at;
+        const int64_t p = split * a.nq * a.hq + at;
         if (l > 0.f || l != l) store_row<float>(a.part + p * a.d + e0, acc, 1.f, a.d - e0, a.d % 4 == 0, h);
         if (h == 0 && dw == 0) a.ml[p] = make_float2(m, l);
     }
@@ -835,7 +838,7 @@ template <int DT, int WAVES> __device__ __forceinline__ void join_waves(char *ld
 
 // dQ, and D for the pass over the keys: the walk of the forward kernel.
 template <typename E, int D, int QW, bool VEC>
-__global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::DIRECT ? 2 : 1)) void attn_bwd_dq_kernel(Args a)
+__global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::AT_ONCE_DQ)) void attn_bwd_dq_kernel(Args a)
 {
     typedef Keys<E, D, QW, VEC> S;
     typedef Tile<E, D> L;
@@ -849,13 +852,10 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     const Place place = place_of(a.qo, a.nq, a.ko, a.nk, a.batch, a.sorted, a.group, S::BQ, slot, lane);
     if (place.tile < 0) return;
     const Span q = place.own, k = place.stream;
-    const int64_t rows = (int64_t)(q.end - q.begin) * a.group, row0 = (int64_t)place.tile * S::BQ;
-
-    const int64_t row = row0 + 32 * qw + (lane & 31);
+    // n_q * heads_q and a tile more are below 2^31
+    const int rows = (q.end - q.begin) * a.group, row = place.tile * S::BQ + 32 * qw + (lane & 31);
     const bool valid = row < rows;
-    const int64_t token = valid ? q.begin + row / a.group : q.begin;
-    const int head = kvh * a.group + (valid ? (int)(row % a.group) : 0);
-    const int64_t at = token * a.hq + head;
+    const int token = q.begin + (valid ? row / a.group : 0), head = kvh * a.group + (valid ? row % a.group : 0), at = token * a.hq + head;
     const int tiles = (k.end - k.begin + S::BK - 1) / S::BK;
     const int t0 = (int)((int64_t)tiles * split / a.splits), t1 = (int)((int64_t)tiles * (split + 1) / a.splits);
     const T *kp = (const T *)a.K + k.begin * a.ld_k + (int64_t)kvh * a.d, *vp = (const T *)a.V + k.begin * a.ld_v + (int64_t)kvh * a.d;
@@ -961,7 +961,7 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
         for (int dt = 0; dt < S::DT; ++dt) acc[dt] = f32x16{};
     const int e0 = 32 * S::DT * dw;
     if (a.splits == 1) store_row<T>((T *)a.dQ + token * a.ld_dq + (int64_t)head * a.d + e0, acc, a.scale, a.d - e0, VEC, h);
-    else store_row<float>(a.part + ((int64_t)split * a.nq * a.hq + at) * a.d + e0, acc, a.scale, a.d - e0, a.d % 4 == 0, h);
+    else store_row<float>(a.part + (split * a.nq * a.hq + at) * a.d + e0, acc, a.scale, a.d - e0, a.d % 4 == 0, h);
 }
 
 // dQ = the sum of its splits, in their order; a thread per element
@@ -985,10 +985,11 @@ template <typename E, int D, int KW, bool VEC> struct Queries {
     static constexpr int PLANE = BR * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE, BUFFER = 2 * TILE + 2 * BR * 4;
     static constexpr int BUFFERS = KW == 1 || 2 * BUFFER > 80 * 1024 ? 1 : 2;
     static constexpr bool DIRECT = VEC && E::PLANES == 1 && KW == 4;
+    static constexpr int AT_ONCE = DIRECT ? (D < 128 ? 2 : 1) : E::PLANES == 3 && KW == 4 && D == 64 ? 2 : 1;   // as above (fp32 of 64 channels 752 -> 716 us)
     static constexpr int JOIN = KW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = BUFFERS * BUFFER > JOIN ? BUFFERS * BUFFER : JOIN;
 };
 template <typename E, int D, int KW, bool VEC>
-__global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, KW, VEC>::DIRECT && D < 128 ? 2 : 1)) void attn_bwd_dkv_kernel(Args a)
+__global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, KW, VEC>::AT_ONCE)) void attn_bwd_dkv_kernel(Args a)
 {
     typedef Queries<E, D, KW, VEC> S;
     typedef Tile<E, D> L;
@@ -1003,7 +1004,7 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
     if (place.tile < 0) return;
     const Span q = place.stream, k = place.own;
 
-    const int64_t key = k.begin + (int64_t)place.tile * S::BK + 32 * kw + (lane & 31);
+    const int key = k.begin + place.tile * S::BK + 32 * kw + (lane & 31);
     const bool valid = key < k.end, seen = valid && (!a.mask || a.mask[key]);
     const int len = q.end - q.begin, tiles = (len + S::BR - 1) / S::BR;
     const int s0 = (int)((int64_t)tiles * a.group * split / a.splits), s1 = (int)((int64_t)tiles * a.group * (split + 1) / a.splits);
@@ -1096,7 +1097,7 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
         store_row<T>((T *)a.dV + key * a.ld_dv + (int64_t)kvh * a.d + e0, dv, 1.f, a.d - e0, VEC, h);
     } else {
         const int64_t rows = a.nk * a.hkv;
-        float *p = a.part + ((int64_t)split * 2 * rows + key * a.hkv + kvh) * a.d + e0;
+        float *p = a.part + (split * 2 * rows + (int64_t)key * a.hkv + kvh) * a.d + e0;
         store_row<float>(p, dk, a.scale, a.d - e0, a.d % 4 == 0, h);
         store_row<float>(p + rows * a.d, dv, 1.f, a.d - e0, a.d % 4 == 0, h);
     }
