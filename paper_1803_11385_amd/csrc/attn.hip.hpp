@@ -985,7 +985,9 @@ template <typename E, int D, int KW, bool VEC> struct Queries {
     static constexpr int PLANE = BR * Tile<E, D>::STRIDE, TILE = E::PLANES * PLANE, BUFFER = 2 * TILE + 2 * BR * 4;
     static constexpr int BUFFERS = KW == 1 || 2 * BUFFER > 80 * 1024 ? 1 : 2;
     static constexpr bool DIRECT = VEC && E::PLANES == 1 && KW == 4;
-    static constexpr int AT_ONCE = DIRECT ? (D < 128 ? 2 : 1) : E::PLANES == 3 && KW == 4 && D == 64 ? 2 : 1;   // as above (fp32 of 64 channels 752 -> 716 us)
+    // fp32 of 64 channels could have two, with 36 registers in scratch: 752 -> 716 us with workgroups for every compute unit twice over, but
+    // 22 -> 35 where each is alone (21 shapes of 4971 rows together, 2 heads of 40)
+    static constexpr int AT_ONCE = DIRECT && D < 128 ? 2 : 1;
     static constexpr int JOIN = KW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = BUFFERS * BUFFER > JOIN ? BUFFERS * BUFFER : JOIN;
 };
 template <typename E, int D, int KW, bool VEC>
