@@ -964,17 +964,6 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     else store_row<float>(a.part + (split * a.nq * a.hq + at) * a.d + e0, acc, a.scale, a.d - e0, a.d % 4 == 0, h);
 }
 
-// dQ = the sum of its splits, in their order; a thread per element
-template <typename T> __global__ __launch_bounds__(256) void attn_bwd_join_kernel(Args a)
-{
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = a.nq * a.hq;
-    if (i >= rows * a.d) return;
-    float t = 0.f;
-    for (int s = 0; s < a.splits; ++s) t += a.part[s * rows * a.d + i];
-    const int64_t at = i / a.d, token = at / a.hq;
-    ((T *)a.dQ)[token * a.ld_dq + (at - token * a.hq) * a.d + (i - at * a.d)] = (T)t;
-}
-
 // dK and dV: a wavefront has 32 keys, the queries of all heads that share their head stream past, one head after
 // the other, so the sum over them is taken in registers in a fixed order.  KW wavefronts have keys of their own (4, wide)
 // or all share 32 keys and deal the queries of a tile among them (1, narrow).
@@ -1105,15 +1094,21 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
     }
 }
 
-// dK and dV = the sums of their splits
-template <typename T> __global__ __launch_bounds__(256) void attn_bwd_join_keys_kernel(Args a)
+// The gradients whose passes were split = the sums of their splits, in their order; a thread per element.  One launch for all three: the
+// first `q_blocks` workgroups have dQ, the others dK and dV (none, where a pass was not split).
+template <typename T> __global__ __launch_bounds__(256) void attn_bwd_join_kernel(Args a, const float *q_part, int q_splits, int q_blocks)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.nk * a.hkv * a.d;
-    if (i >= 2 * n) return;
+    const bool query = (int)blockIdx.x < q_blocks;
+    const int64_t i = (int64_t)(blockIdx.x - (query ? 0 : q_blocks)) * 256 + threadIdx.x;
+    const int heads = query ? a.hq : a.hkv, splits = query ? q_splits : a.splits;
+    const int64_t n = (query ? a.nq : a.nk) * heads * a.d, all = query ? n : 2 * n;       // dK, then dV
+    if (i >= all) return;
+    const float *p = (query ? q_part : a.part) + i;
     float t = 0.f;
-    for (int s = 0; s < a.splits; ++s) t += a.part[s * 2 * n + i];
-    const int64_t e = i < n ? i : i - n, at = e / a.d, row = at / a.hkv, col = (at - row * a.hkv) * a.d + (e - at * a.d);
-    if (i < n) ((T *)a.dK)[row * a.ld_dk + col] = (T)t;
+    for (int s = 0; s < splits; ++s) t += p[s * all];
+    const int64_t e = i < n ? i : i - n, at = e / a.d, row = at / heads, col = (at - row * heads) * a.d + (e - at * a.d);
+    if (query) ((T *)a.dQ)[row * a.ld_dq + col] = (T)t;
+    else if (i < n) ((T *)a.dK)[row * a.ld_dk + col] = (T)t;
     else ((T *)a.dV)[row * a.ld_dv + col] = (T)t;
 }
 

@@ -91,10 +91,9 @@ size_t key_part_bytes(const hch_attn_desc &p, int splits) { return splits > 1 ? 
 size_t delta_bytes(const hch_attn_desc &p) { return round256((size_t)p.n_q * p.heads_q * 4); }
 
 size_t fwd_bytes(const hch_attn_desc &p, const Plan &r) { return std::max<size_t>(256, part_bytes(p, r.splits) + ml_bytes(p, r.splits)); }
-// the parts of dQ are joined before those of dK and dV are written
 size_t bwd_bytes(const hch_attn_desc &p, const Plan &dq, const Plan &dkv)
 {
-    return delta_bytes(p) + std::max<size_t>({256, part_bytes(p, dq.splits), key_part_bytes(p, dkv.splits)});
+    return std::max<size_t>(256, delta_bytes(p) + part_bytes(p, dq.splits) + key_part_bytes(p, dkv.splits));
 }
 
 constexpr int64_t ROWS = 0x7fffffff - 256;              // the last tile's end is an int too
@@ -210,7 +209,8 @@ try {
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse = const_cast<float *>(lse); a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV;
     a.vec = whole(p, {Q, K, V, O, dO, dQ, dK, dV}, {p.ld_q, p.ld_k, p.ld_v, p.ld_o, p.ld_do, p.ld_dq, p.ld_dk, p.ld_dv});
     a.delta = (float *)workspace;
-    a.part = (float *)((char *)workspace + delta_bytes(p));
+    float *const q_part = (float *)((char *)workspace + delta_bytes(p));
+    a.part = q_part;
     const hipStream_t s = (hipStream_t)stream;
     if (p.n_q) {
         a.slots = (int)rq.slots; a.splits = rq.splits; hch::attn::set_work(a);
@@ -220,11 +220,15 @@ try {
         if (st != HCH_OK) return st;
     }
     if (p.n_k) {
+        a.part = (float *)((char *)q_part + part_bytes(p, rq.splits));
         a.slots = (int)rk.slots; a.splits = rk.splits; hch::attn::set_work(a);
         const double bytes = row_bytes(p, 2, 4), flops = 8 * pairs(p);
         st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dkv<float>(a, rk.narrow, bytes, flops, s)
                                 : hch::attn::launch_bwd_dkv<__bf16>(a, rk.narrow, bytes, flops, s);
+        if (st != HCH_OK) return st;
     }
+    if (rq.splits > 1 || (p.n_k && rk.splits > 1))
+        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_join<float>(a, q_part, rq.splits, s) : hch::attn::launch_bwd_join<__bf16>(a, q_part, rq.splits, s);
     return st;
 } catch (const std::exception &) {
     return HCH_ENOMEM;

@@ -13,6 +13,8 @@ namespace attn {
 template <typename T> hch_status launch_fwd(const Args &a, bool narrow, double bytes, double flops, hipStream_t s);
 template <typename T> hch_status launch_bwd_dq(const Args &a, bool narrow, double bytes, double flops, hipStream_t s);
 template <typename T> hch_status launch_bwd_dkv(const Args &a, bool narrow, double bytes, double flops, hipStream_t s);
+// dQ from its splits, and dK and dV from theirs (those of `a`); 1 split: written already
+template <typename T> hch_status launch_bwd_join(const Args &a, const float *q_part, int q_splits, hipStream_t s);
 
 #ifdef HCH_ATTN_TYPE
 template <typename T> struct EngineOf { typedef Bf16 E; };
@@ -101,15 +103,6 @@ template <typename T> hch_status launch_bwd_dq(const Args &a, bool narrow, doubl
         }
     });
     HCH_LAUNCH_CHECK("attn_bwd_dq_kernel");
-    if (a.splits > 1) {
-        {
-            static const int id = join_id("attn::attn_bwd_join_kernel", TYPE_NAME<T>, 0);
-            LaunchTimer lt(id, s, (double)a.splits * a.nq * a.hq * 4 * a.d, 0.0);
-            constexpr auto kernel = attn_bwd_join_kernel<T>;
-            HCH_LAUNCH(kernel, dim3((unsigned)((a.nq * a.hq * a.d + 255) / 256)), dim3(256), 0, s, a);
-        }
-        HCH_LAUNCH_CHECK("attn_bwd_join_kernel");
-    }
     return HCH_OK;
 }
 
@@ -132,21 +125,24 @@ template <typename T> hch_status launch_bwd_dkv(const Args &a, bool narrow, doub
         }
     });
     HCH_LAUNCH_CHECK("attn_bwd_dkv_kernel");
-    if (a.splits > 1) {
-        {
-            static const int id = join_id("attn::attn_bwd_join_keys_kernel", TYPE_NAME<T>, 0);
-            LaunchTimer lt(id, s, (double)a.splits * a.nk * a.hkv * 8 * a.d, 0.0);
-            constexpr auto kernel = attn_bwd_join_keys_kernel<T>;
-            HCH_LAUNCH(kernel, dim3((unsigned)((2 * a.nk * a.hkv * a.d + 255) / 256)), dim3(256), 0, s, a);
-        }
-        HCH_LAUNCH_CHECK("attn_bwd_join_keys_kernel");
-    }
+    return HCH_OK;
+}
+
+template <typename T> hch_status launch_bwd_join(const Args &a, const float *q_part, int q_splits, hipStream_t s)
+{
+    const int64_t nq = q_splits > 1 ? a.nq * a.hq * a.d : 0, nk = a.splits > 1 ? 2 * a.nk * a.hkv * a.d : 0, blocks = (nq + 255) / 256;
+    static const int id = join_id("attn::attn_bwd_join_kernel", TYPE_NAME<T>, 0);
+    LaunchTimer lt(id, s, 4.0 * ((double)q_splits * nq + (double)a.splits * nk), 0.0);
+    constexpr auto kernel = attn_bwd_join_kernel<T>;
+    HCH_LAUNCH(kernel, dim3((unsigned)(blocks + (nk + 255) / 256)), dim3(256), 0, s, a, q_part, q_splits, (int)blocks);
+    HCH_LAUNCH_CHECK("attn_bwd_join_kernel");
     return HCH_OK;
 }
 
 template hch_status launch_fwd<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
 template hch_status launch_bwd_dq<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
 template hch_status launch_bwd_dkv<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
+template hch_status launch_bwd_join<HCH_ATTN_TYPE>(const Args &, const float *, int, hipStream_t);
 #endif
 
 }  // namespace attn

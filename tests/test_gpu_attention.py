@@ -167,7 +167,7 @@ def test_both_forms_of_every_width(dtype, pad, d):
 def test_splits_of_every_pass_are_joined():
     c = Case("f32", [900], [1100], 1, 1, 96, masked=0.1, seed=8)
     names = _launched(c.run)
-    for part in ("attn_join_kernel<float, ", "attn_bwd_join_kernel<float>", "attn_bwd_join_keys_kernel<float>"):
+    for part in ("attn_join_kernel<float, ", "attn_bwd_join_kernel<float>"):
         assert any(part in n for n in names), names
     c.check()
     c = Case("bf16", [1], [60000], 2, 1, 128, seed=9)
