@@ -837,16 +837,14 @@ template <int DT, int WAVES> __device__ __forceinline__ void join_waves(char *ld
 }
 
 // dQ, and D for the pass over the keys: the walk of the forward kernel.
-template <typename E, int D, int QW, bool VEC>
-__global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::AT_ONCE_DQ)) void attn_bwd_dq_kernel(Args a)
+template <typename E, int D, int QW, bool VEC> __device__ __forceinline__ void bwd_dq(const Args &a, int id, char *lds)
 {
     typedef Keys<E, D, QW, VEC> S;
     typedef Tile<E, D> L;
     typedef typename E::T T;
-    __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int qw = QW == 1 ? 0 : wave, kw = QW == 1 ? wave % S::KW : 0, dw = QW == 1 ? wave / S::KW : 0;
-    const Work w = work_of(a, blockIdx.x);
+    const Work w = work_of(a, id);
     const int split = w.split, slot = w.slot, kvh = w.head;
     if (slot >= a.slots) return;
     const Place place = place_of(a.qo, a.nq, a.ko, a.nk, a.batch, a.sorted, a.group, S::BQ, slot, lane);
@@ -932,7 +930,7 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     grad.load(gp, valid, a.d, VEC, h);
     float delta = row_dot<T, D>(gp, (const T *)a.O + token * a.ld_o + (int64_t)head * a.d, valid, a.d, VEC, h);
     if (!part) delta = 0.f;
-    if (valid && split == 0 && kw == 0 && dw == 0 && h == 0) a.delta[at] = delta;
+    if (a.delta && valid && split == 0 && kw == 0 && dw == 0 && h == 0) a.delta[at] = delta;
     for (int t = t0; t < t1; ++t) {
         char *kt = buffer(t), *vt = kt + S::TILE;
         arrive(t);
@@ -964,6 +962,13 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
     else store_row<float>(a.part + (split * a.nq * a.hq + at) * a.d + e0, acc, a.scale, a.d - e0, a.d % 4 == 0, h);
 }
 
+template <typename E, int D, int QW, bool VEC>
+__global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::AT_ONCE_DQ)) void attn_bwd_dq_kernel(Args a)
+{
+    __shared__ __align__(16) char lds[Keys<E, D, QW, VEC>::LDS];
+    bwd_dq<E, D, QW, VEC>(a, blockIdx.x, lds);
+}
+
 // dK and dV: a wavefront has 32 keys, the queries of all heads that share their head stream past, one head after
 // the other, so the sum over them is taken in registers in a fixed order.  KW wavefronts have keys of their own (4, wide)
 // or all share 32 keys and deal the queries of a tile among them (1, narrow).
@@ -979,16 +984,14 @@ template <typename E, int D, int KW, bool VEC> struct Queries {
     static constexpr int AT_ONCE = DIRECT && D < 128 ? 2 : 1;
     static constexpr int JOIN = KW == 1 ? WAVES * 32 * (32 * DT + 4) * 4 : 0, LDS = BUFFERS * BUFFER > JOIN ? BUFFERS * BUFFER : JOIN;
 };
-template <typename E, int D, int KW, bool VEC>
-__global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, KW, VEC>::AT_ONCE)) void attn_bwd_dkv_kernel(Args a)
+template <typename E, int D, int KW, bool VEC> __device__ __forceinline__ void bwd_dkv(const Args &a, int id, char *lds)
 {
     typedef Queries<E, D, KW, VEC> S;
     typedef Tile<E, D> L;
     typedef typename E::T T;
-    __shared__ __align__(16) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int kw = KW == 1 ? 0 : wave, qw = KW == 1 ? wave % S::QW : 0, dw = KW == 1 ? wave / S::QW : 0;
-    const Work w = work_of(a, blockIdx.x);
+    const Work w = work_of(a, id);
     const int split = w.split, slot = w.slot, kvh = w.head;
     if (slot >= a.slots) return;
     const Place place = place_of(a.ko, a.nk, a.qo, a.nq, a.batch, a.sorted, 1, S::BK, slot, lane);
@@ -1092,6 +1095,45 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
         store_row<float>(p, dk, a.scale, a.d - e0, a.d % 4 == 0, h);
         store_row<float>(p + rows * a.d, dv, 1.f, a.d - e0, a.d % 4 == 0, h);
     }
+}
+
+template <typename E, int D, int KW, bool VEC>
+__global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, KW, VEC>::AT_ONCE)) void attn_bwd_dkv_kernel(Args a)
+{
+    __shared__ __align__(16) char lds[Queries<E, D, KW, VEC>::LDS];
+    bwd_dkv<E, D, KW, VEC>(a, blockIdx.x, lds);
+}
+
+// Both passes in one launch, for calls neither of which fills the compute units: the first `q_grid` workgroups form dQ, the others dK
+// and dV, from a D that attn_delta_kernel left.
+template <typename E, int D, int W> struct Both {
+    typedef Keys<E, D, W, true> K;
+    typedef Queries<E, D, W, true> Q;
+    static constexpr int AT_ONCE = K::AT_ONCE_DQ < Q::AT_ONCE ? K::AT_ONCE_DQ : Q::AT_ONCE, LDS = K::LDS > Q::LDS ? K::LDS : Q::LDS;
+};
+template <typename E, int D, int W>
+__global__ __launch_bounds__((Keys<E, D, W, true>::THREADS), (Both<E, D, W>::AT_ONCE)) void attn_bwd_both_kernel(Args a, Args b, int q_grid)
+{
+    __shared__ __align__(16) char lds[Both<E, D, W>::LDS];
+    if ((int)blockIdx.x < q_grid) bwd_dq<E, D, W, true>(a, blockIdx.x, lds);
+    else bwd_dkv<E, D, W, true>(b, blockIdx.x - q_grid, lds);
+}
+// D of every row, by `lanes` lanes (a power of two) of 16 bytes a row; 0 where the row saw no key
+template <typename T> __global__ __launch_bounds__(256) void attn_delta_kernel(Args a, int lanes)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
+    const int lane = threadIdx.x % lanes, e = lane * N;
+    if (at >= a.nq * a.hq) return;                      // (whole groups of lanes)
+    const int64_t token = at / a.hq, head = at - token * a.hq;
+    T x[N], y[N];
+    load_piece((const T *)a.dO + token * a.ld_do + head * a.d, e, true, a.d, true, x);
+    load_piece((const T *)a.O + token * a.ld_o + head * a.d, e, true, a.d, true, y);
+    float t = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) t += (float)x[j] * (float)y[j];
+    for (int i = 1; i < lanes; i <<= 1) t += __shfl_xor(t, i);
+    if (lane == 0) a.delta[at] = a.lse[at] == -INFINITY ? 0.f : t;
 }
 
 // The gradients whose passes were split = the sums of their splits, in their order; a thread per element.  One launch for all three: the

@@ -18,6 +18,11 @@ struct Plan {
     bool narrow;           // tiles of 32 rows (keys) whose wavefronts share what streams past, not of 128
     int splits;            // parts of what streams past, joined by a second launch
     int64_t slots;
+    double us, workgroups; // what it takes by the reckoning below, and about how many have work
+};
+struct Plans {             // the best one with wide tiles and with narrow ones
+    Plan form[2];
+    const Plan &best() const { return form[form[1].us < form[0].us]; }
 };
 
 // What a pass takes, as a sum of steps (64 streamed rows in bf16, 32 in fp32; narrow 128, and 64 in fp32 beyond 64 channels):
@@ -35,11 +40,11 @@ constexpr double START = 5.3, JOIN = 5.7, FWD = 1.0, DQ = 1.33, DKV = 1.45, JOIN
 // rows: of the tiles, over all shapes, `heads` times; stream: rows that one of those tiles sees on average; width: bytes of a
 // row's partial sums; moved: bytes of what streams past, all of it once.  Offsets are known on the device only, so
 // shapes count as equal, the longest as UNEVEN times the mean.
-Plan plan(const hch_attn_desc &p, int64_t rows, int heads, double stream, double cost, double width, double moved)
+Plans plan(const hch_attn_desc &p, int64_t rows, int rows_each, int heads, double stream, double cost, double width, double moved)
 {
     const int type = p.dtype == HCH_BF16, dc = std::min(3, (p.head_dim - 1) / 32);
-    Plan best = {false, 1, 0};
-    double least = 0.0;
+    Plans r = {};
+    rows *= rows_each;
     for (int narrow = 0; narrow < 2; ++narrow) {
         const Step &st = STEP[type][narrow][dc];
         const int size = narrow ? 32 : 128, step = narrow ? (!type && dc >= 2 ? 64 : 128) : type ? 64 : 32;
@@ -58,30 +63,48 @@ Plan plan(const hch_attn_desc &p, int64_t rows, int heads, double stream, double
             const double move = moved / MEMORY * each * UNITS / (wgs * splits) * share;
             us = std::max(us, move) + 0.2 * std::min(us, move);         // (they do not overlap altogether)
             if (splits > 1) us += JOIN + JOIN_SPLIT * splits + 2.0 * splits * rows * heads * width / BYTES_PER_US;
-            if (best.slots == 0 || us < least) {
-                least = us;
-                best = {narrow != 0, splits, 1};
-            }
+            if (i == 0 || us < r.form[narrow].us) r.form[narrow] = {narrow != 0, splits, 0, us, wgs * splits};
         }
+        r.form[narrow].slots = hch::attn::slots_of(rows / rows_each, rows_each, size, p.batch);
     }
-    return best;
+    return r;
 }
 
 double row_bytes(const hch_attn_desc &p, int q, int k) { return (double)size_of(p.dtype) * p.head_dim * ((double)q * p.n_q * p.heads_q + (double)k * p.n_k * p.heads_kv); }
 
-Plan plan_keys(const hch_attn_desc &p, double cost)     // forward and dQ: tiles of query rows, keys stream past
+Plans plan_keys(const hch_attn_desc &p, double cost)    // forward and dQ: tiles of query rows, keys stream past
 {
-    const int group = p.heads_q / p.heads_kv;
-    Plan r = plan(p, p.n_q * group, p.heads_kv, (double)p.n_k / p.batch, cost, 4.0 * p.head_dim, row_bytes(p, 0, 2));
-    r.slots = hch::attn::slots_of(p.n_q, group, r.narrow ? 32 : 128, p.batch);
-    return r;
+    return plan(p, p.n_q, p.heads_q / p.heads_kv, p.heads_kv, (double)p.n_k / p.batch, cost, 4.0 * p.head_dim, row_bytes(p, 0, 2));
 }
 
-Plan plan_queries(const hch_attn_desc &p)               // dK and dV: tiles of keys, the queries of a head's group stream past
+Plans plan_queries(const hch_attn_desc &p)              // dK and dV: tiles of keys, the queries of a head's group stream past
 {
-    const int group = p.heads_q / p.heads_kv;
-    Plan r = plan(p, p.n_k, p.heads_kv, (double)p.n_q / p.batch * group, DKV, 8.0 * p.head_dim, row_bytes(p, 2, 0));
-    r.slots = hch::attn::slots_of(p.n_k, 1, r.narrow ? 32 : 128, p.batch);
+    return plan(p, p.n_k, 1, p.heads_kv, (double)p.n_q / p.batch * (p.heads_q / p.heads_kv), DKV, 8.0 * p.head_dim, row_bytes(p, 2, 0));
+}
+
+// The backward pass: dQ, then dK and dV, each with the tiles that are best for it; or, in whole pieces, both in one launch where all their
+// workgroups find room on the compute units at once, after a launch that takes START for D.  ROOM: workgroups of a compute unit by type,
+// form and head width, from the kernels' registers.  (Of 70 batches the 39 within that room took 0.74 of the two
+// launches' time in the mean, 0.61 to 1.01; most of those beyond it would take as long either way.)
+constexpr int ROOM[2][2][4] = {{{2, 1, 1, 1}, {2, 1, 1, 1}}, {{4, 2, 2, 1}, {3, 2, 1, 1}}};
+struct Backward {
+    Plan dq, dkv;          // two launches
+    Plan dq1, dkv1;        // one
+    bool together;
+};
+Backward plan_backward(const hch_attn_desc &p)
+{
+    const Plans q = plan_keys(p, DQ), k = plan_queries(p);
+    Backward r = {q.best(), k.best(), {}, {}, false};
+    double least = r.dq.us + r.dkv.us;
+    for (int narrow = 0; narrow < 2; ++narrow) {
+        const int room = ROOM[p.dtype == HCH_BF16][narrow][std::min(3, (p.head_dim - 1) / 32)];
+        const double us = START + std::max(q.form[narrow].us, k.form[narrow].us);
+        if (q.form[narrow].workgroups + k.form[narrow].workgroups > room * UNITS || us >= least) continue;
+        least = us;
+        r.dq1 = q.form[narrow]; r.dkv1 = k.form[narrow];
+        r.together = true;
+    }
     return r;
 }
 
@@ -91,9 +114,10 @@ size_t key_part_bytes(const hch_attn_desc &p, int splits) { return splits > 1 ? 
 size_t delta_bytes(const hch_attn_desc &p) { return round256((size_t)p.n_q * p.heads_q * 4); }
 
 size_t fwd_bytes(const hch_attn_desc &p, const Plan &r) { return std::max<size_t>(256, part_bytes(p, r.splits) + ml_bytes(p, r.splits)); }
-size_t bwd_bytes(const hch_attn_desc &p, const Plan &dq, const Plan &dkv)
+size_t bwd_bytes(const hch_attn_desc &p, const Backward &r)         // whichever it will be
 {
-    return std::max<size_t>(256, delta_bytes(p) + part_bytes(p, dq.splits) + key_part_bytes(p, dkv.splits));
+    const auto bytes = [&](const Plan &dq, const Plan &dkv) { return part_bytes(p, dq.splits) + key_part_bytes(p, dkv.splits); };
+    return std::max<size_t>(256, delta_bytes(p) + std::max(bytes(r.dq, r.dkv), r.together ? bytes(r.dq1, r.dkv1) : 0));
 }
 
 constexpr int64_t ROWS = 0x7fffffff - 256;              // the last tile's end is an int too
@@ -160,7 +184,7 @@ extern "C" size_t hch_attn_workspace_bytes(const hch_attn_desc *desc, hch_ws_kin
 try {
     if (check_sizes("hch_attn_workspace_bytes", desc) != HCH_OK || (kind != HCH_WS_FWD && kind != HCH_WS_BWD_DATA)) return 0;
     if (!desc->n_q) return 256;
-    return kind == HCH_WS_FWD ? fwd_bytes(*desc, plan_keys(*desc, FWD)) : bwd_bytes(*desc, plan_keys(*desc, DQ), plan_queries(*desc));
+    return kind == HCH_WS_FWD ? fwd_bytes(*desc, plan_keys(*desc, FWD).best()) : bwd_bytes(*desc, plan_backward(*desc));
 } catch (const std::exception &) {
     return 0;
 }
@@ -171,7 +195,7 @@ try {
     hch_status st = check_sizes("hch_attn_fwd", desc);
     if (st != HCH_OK) return st;
     const hch_attn_desc &p = *desc;
-    const Plan r = p.n_q ? plan_keys(p, FWD) : Plan{false, 1, 0};
+    const Plan r = p.n_q ? plan_keys(p, FWD).best() : Plan{false, 1, 0, 0.0, 0.0};
     st = check_call("hch_attn_fwd", desc, workspace, ws_bytes, fwd_bytes(p, r));
     if (st != HCH_OK) return st;
     if ((p.n_q && (!Q || !O)) || (p.n_k && (!K || !V))) return fail(HCH_EINVAL, "hch_attn_fwd: null pointer");
@@ -196,39 +220,50 @@ try {
     hch_status st = check_sizes("hch_attn_bwd", desc);
     if (st != HCH_OK) return st;
     const hch_attn_desc &p = *desc;
-    const Plan none = {false, 1, p.batch ? hch::attn::slots_of(p.n_k, 1, 128, p.batch) : 0};       // without queries: zeros
-    const Plan rq = p.n_q ? plan_keys(p, DQ) : none, rk = p.n_q ? plan_queries(p) : none;
-    st = check_call("hch_attn_bwd", desc, workspace, ws_bytes, p.n_q ? bwd_bytes(p, rq, rk) : 256);
+    const Plan none = {false, 1, p.batch ? hch::attn::slots_of(p.n_k, 1, 128, p.batch) : 0, 0.0, 0.0};       // without queries: zeros
+    const Backward r = p.n_q ? plan_backward(p) : Backward{none, none, {}, {}, false};
+    st = check_call("hch_attn_bwd", desc, workspace, ws_bytes, p.n_q ? bwd_bytes(p, r) : 256);
     if (st != HCH_OK) return st;
     const int64_t wq = (int64_t)p.heads_q * p.head_dim, wk = (int64_t)p.heads_kv * p.head_dim;
     if (p.ld_do < wq || p.ld_dq < wq || p.ld_dk < wk || p.ld_dv < wk) return fail(HCH_EINVAL, "hch_attn_bwd: row stride below a row's length");
     if (std::max({p.ld_do, p.ld_dq, p.ld_dk, p.ld_dv}) >= 1 << 22) return fail(HCH_EUNSUPPORTED, "hch_attn_bwd: row stride of 2^22 elements or more");
     if ((p.n_q && (!Q || !O || !lse || !dO || !dQ)) || (p.n_k && (!K || !V || !dK || !dV))) return fail(HCH_EINVAL, "hch_attn_bwd: null pointer");
-    if (!launchable(p, rq) || !launchable(p, rk)) return fail(HCH_EUNSUPPORTED, "hch_attn_bwd: too many rows for one launch");
+    if (!launchable(p, r.dq) || !launchable(p, r.dkv)) return fail(HCH_EUNSUPPORTED, "hch_attn_bwd: too many rows for one launch");
     Args a = args_of(p);
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse = const_cast<float *>(lse); a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV;
     a.vec = whole(p, {Q, K, V, O, dO, dQ, dK, dV}, {p.ld_q, p.ld_k, p.ld_v, p.ld_o, p.ld_do, p.ld_dq, p.ld_dk, p.ld_dv});
     a.delta = (float *)workspace;
+    const bool together = r.together && a.vec && p.n_k;
+    const Plan &rq = together ? r.dq1 : r.dq, &rk = together ? r.dkv1 : r.dkv;
     float *const q_part = (float *)((char *)workspace + delta_bytes(p));
     a.part = q_part;
     const hipStream_t s = (hipStream_t)stream;
-    if (p.n_q) {
-        a.slots = (int)rq.slots; a.splits = rq.splits; hch::attn::set_work(a);
-        const double bytes = row_bytes(p, 4, 2), flops = 6 * pairs(p);
-        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dq<float>(a, rq.narrow, bytes, flops, s)
-                                : hch::attn::launch_bwd_dq<__bf16>(a, rq.narrow, bytes, flops, s);
+    Args b = a;
+    b.part = (float *)((char *)q_part + part_bytes(p, rq.splits));
+    a.slots = (int)rq.slots; a.splits = rq.splits; hch::attn::set_work(a);
+    b.slots = (int)rk.slots; b.splits = rk.splits; hch::attn::set_work(b);
+    if (together) {
+        a.delta = nullptr;                              // D is there already
+        const double bytes = row_bytes(p, 5, 6), flops = 14 * pairs(p);
+        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_both<float>(a, b, rq.narrow, bytes, flops, s)
+                                : hch::attn::launch_bwd_both<__bf16>(a, b, rq.narrow, bytes, flops, s);
         if (st != HCH_OK) return st;
-    }
-    if (p.n_k) {
-        a.part = (float *)((char *)q_part + part_bytes(p, rq.splits));
-        a.slots = (int)rk.slots; a.splits = rk.splits; hch::attn::set_work(a);
-        const double bytes = row_bytes(p, 2, 4), flops = 8 * pairs(p);
-        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dkv<float>(a, rk.narrow, bytes, flops, s)
-                                : hch::attn::launch_bwd_dkv<__bf16>(a, rk.narrow, bytes, flops, s);
-        if (st != HCH_OK) return st;
+    } else {
+        if (p.n_q) {
+            const double bytes = row_bytes(p, 4, 2), flops = 6 * pairs(p);
+            st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dq<float>(a, rq.narrow, bytes, flops, s)
+                                    : hch::attn::launch_bwd_dq<__bf16>(a, rq.narrow, bytes, flops, s);
+            if (st != HCH_OK) return st;
+        }
+        if (p.n_k) {
+            const double bytes = row_bytes(p, 2, 4), flops = 8 * pairs(p);
+            st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_dkv<float>(b, rk.narrow, bytes, flops, s)
+                                    : hch::attn::launch_bwd_dkv<__bf16>(b, rk.narrow, bytes, flops, s);
+            if (st != HCH_OK) return st;
+        }
     }
     if (rq.splits > 1 || (p.n_k && rk.splits > 1))
-        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_join<float>(a, q_part, rq.splits, s) : hch::attn::launch_bwd_join<__bf16>(a, q_part, rq.splits, s);
+        st = p.dtype == HCH_F32 ? hch::attn::launch_bwd_join<float>(b, q_part, rq.splits, s) : hch::attn::launch_bwd_join<__bf16>(b, q_part, rq.splits, s);
     return st;
 } catch (const std::exception &) {
     return HCH_ENOMEM;

@@ -13,6 +13,8 @@ namespace attn {
 template <typename T> hch_status launch_fwd(const Args &a, bool narrow, double bytes, double flops, hipStream_t s);
 template <typename T> hch_status launch_bwd_dq(const Args &a, bool narrow, double bytes, double flops, hipStream_t s);
 template <typename T> hch_status launch_bwd_dkv(const Args &a, bool narrow, double bytes, double flops, hipStream_t s);
+// dQ (a) and dK, dV (b) in one launch, after one for D; both `narrow` or not, everything in whole pieces
+template <typename T> hch_status launch_bwd_both(const Args &a, const Args &b, bool narrow, double bytes, double flops, hipStream_t s);
 // dQ from its splits, and dK and dV from theirs (those of `a`); 1 split: written already
 template <typename T> hch_status launch_bwd_join(const Args &a, const float *q_part, int q_splits, hipStream_t s);
 
@@ -37,6 +39,12 @@ inline int instance_id(const char *kernel, const char *engine, int d, int form, 
 {
     char name[96];
     snprintf(name, sizeof name, "%s<%s, %d, %d, %s>", kernel, engine, d, form, vec ? "true" : "false");
+    return Profiler::get().id_for(name);
+}
+inline int both_id(const char *engine, int d, int form)
+{
+    char name[96];
+    snprintf(name, sizeof name, "attn::attn_bwd_both_kernel<%s, %d, %d>", engine, d, form);
     return Profiler::get().id_for(name);
 }
 template <typename T> constexpr const char *TYPE_NAME = sizeof(T) == 4 ? "float" : "__bf16";
@@ -128,6 +136,37 @@ template <typename T> hch_status launch_bwd_dkv(const Args &a, bool narrow, doub
     return HCH_OK;
 }
 
+template <typename T> hch_status launch_bwd_both(const Args &a, const Args &b, bool narrow, double bytes, double flops, hipStream_t s)
+{
+    {
+        const int64_t rows = a.nq * a.hq;
+        int lanes = 1;
+        while (lanes * 16 < a.d * (int)sizeof(T)) lanes *= 2;
+        static const int id = join_id("attn::attn_delta_kernel", TYPE_NAME<T>, 0);
+        LaunchTimer lt(id, s, (double)rows * (2 * a.d * sizeof(T) + 8), 0.0);
+        constexpr auto kernel = attn_delta_kernel<T>;
+        HCH_LAUNCH(kernel, dim3((unsigned)((rows * lanes + 255) / 256)), dim3(256), 0, s, b, lanes);
+    }
+    HCH_LAUNCH_CHECK("attn_delta_kernel");
+    with_width<T>(a.d, narrow, true, [&](auto w, auto) {
+        typedef typename EngineOf<T>::E E;
+        constexpr int D = decltype(w)::value;
+        if (!narrow) {
+            static const int id = both_id(E::NAME, D, 4);
+            constexpr auto kernel = attn_bwd_both_kernel<E, D, 4>;
+            LaunchTimer lt(id, s, bytes, flops);
+            HCH_LAUNCH(kernel, dim3(work_grid(a) + work_grid(b)), dim3((Keys<E, D, 4, true>::THREADS)), 0, s, a, b, (int)work_grid(a));
+        } else if constexpr (has_narrow<T, D>) {
+            static const int id = both_id(E::NAME, D, 1);
+            constexpr auto kernel = attn_bwd_both_kernel<E, D, 1>;
+            LaunchTimer lt(id, s, bytes, flops);
+            HCH_LAUNCH(kernel, dim3(work_grid(a) + work_grid(b)), dim3((Keys<E, D, 1, true>::THREADS)), 0, s, a, b, (int)work_grid(a));
+        }
+    });
+    HCH_LAUNCH_CHECK("attn_bwd_both_kernel");
+    return HCH_OK;
+}
+
 template <typename T> hch_status launch_bwd_join(const Args &a, const float *q_part, int q_splits, hipStream_t s)
 {
     const int64_t nq = q_splits > 1 ? a.nq * a.hq * a.d : 0, nk = a.splits > 1 ? 2 * a.nk * a.hkv * a.d : 0, blocks = (nq + 255) / 256;
@@ -142,6 +181,7 @@ template <typename T> hch_status launch_bwd_join(const Args &a, const float *q_p
 template hch_status launch_fwd<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
 template hch_status launch_bwd_dq<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
 template hch_status launch_bwd_dkv<HCH_ATTN_TYPE>(const Args &, bool, double, double, hipStream_t);
+template hch_status launch_bwd_both<HCH_ATTN_TYPE>(const Args &, const Args &, bool, double, double, hipStream_t);
 template hch_status launch_bwd_join<HCH_ATTN_TYPE>(const Args &, const float *, int, hipStream_t);
 #endif
 

@@ -148,12 +148,14 @@ def _launched(run):
 @pytest.mark.parametrize("d", [24, 64, 96, 128])
 def test_both_forms_of_every_width(dtype, pad, d):
     """Many shapes take tiles of 128 rows, few queries or keys tiles of 32; with addresses and strides in whole pieces and
-    without."""
+    without; both passes of the gradient apart and in one launch."""
     many, some = [100 + 7 * (i % 13) for i in range(70)], [260 + 9 * (i % 5) for i in range(20)]
     names = set()
     for lq, lk, hq, hkv in ((many, many, 4, 2), (some, some, 4, 2), ([1, 2], [1500, 700], 4, 2), ([1300, 40], [20, 3], 4, 2),
                             ([38], [38], 4, 2), ([61], [61], 1, 1), ([43], [43], 4, 2), ([18], [18], 16, 4), ([71, 71], [113, 113], 16, 8),
-                            ([57] * 3, [57] * 3, 8, 4), ([241, 241], [241, 241], 8, 8)):
+                            ([57] * 3, [57] * 3, 8, 4), ([241, 241], [241, 241], 8, 8), ([1] * 83, [7] * 83, 8, 8), ([89] * 4, [111] * 4, 8, 8),
+                            ([237] * 29, [6] * 29, 8, 8), ([1] * 47, [411] * 47, 4, 4), ([1, 1], [855, 855], 1, 1), ([128, 128], [56, 56], 1, 1),
+                            ([3] * 87, [5] * 87, 64, 8)):
         c = Case(dtype, lq, lk, hq, hkv, d, masked=0.1, pad=pad, junk=True, seed=d + pad)
         names |= set(_launched(c.run))
         c.check()
@@ -162,6 +164,7 @@ def test_both_forms_of_every_width(dtype, pad, d):
     for kernel in ("attn_fwd_kernel", "attn_bwd_dq_kernel", "attn_bwd_dkv_kernel"):
         for width, form in (((d + 31) // 32 * 32, 4), (narrow, 1)):
             assert f"attn::{kernel}<attn::{engine}, {width}, {form}, {whole}>" in names, (kernel, form, sorted(names))
+            assert pad or f"attn::attn_bwd_both_kernel<attn::{engine}, {width}, {form}>" in names, (form, sorted(names))
 
 
 def test_splits_of_every_pass_are_joined():
