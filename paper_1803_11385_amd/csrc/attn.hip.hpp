@@ -5,8 +5,9 @@
 //   backward  p_ij = exp(s_ij - lse_i);  D_i = dO_i . o_i;  dS_ij = p_ij (dO_i . v_j - D_i)
 //             dV_j = sum_i p_ij dO_i;  dK_j = scale sum_i dS_ij q_i;  dQ_i = scale sum_j dS_ij k_j
 //
-// All kernels multiply 32 x 32 tiles with the 32x32x16 bf16 instruction.  The scores are always formed so that what stays fixed for a wavefront (its queries, or in the pass over keys its keys)
-// is the column, i.e. the lane, and what streams past is the row, i.e. the register.  Then
+// All kernels multiply 32 x 32 tiles with the 32x32x16 bf16 instruction.  The scores are always formed so that what stays
+// fixed for a wavefront (its queries, or in the pass over keys its keys) is the column, i.e. the lane, and what
+// streams past is the row, i.e. the register.  Then
 //   * a row's maximum and sum are sums over a lane's own registers and one exchange between the two
 //     half-wavefronts, and what scales a query is one number per lane;
 //   * the probabilities are already laid out as the right operand of the second product, whose reduction runs
@@ -532,7 +533,13 @@ template <typename E, int D, int QW, bool VEC> struct Keys {
 // forward
 // ---------------------------------------------------------------------------------------------
 // Query rows of the heads that share a key head are one list, row = token * group + (head within the group), so that
-// a tile of keys serves the whole group.
+// a tile of keys serves the whole group.  The weights p (0 to 2^8) are rounded to bf16 where the second product takes them (in three
+// parts with fp32); their sum l is of what they were before.
+// Bound by the matrix pipes and the softmax between the products: at 64 channels the pipes work 0.45 of the time, at 128 0.56, and the vector
+// units most of the rest.  bf16, 16 shapes of 4096, 16 heads of 32 / 64 / 96 / 128 channels: 947 / 1225 / 1630 / 2100 us, 580 / 900 / 1010 /
+// 1050 TFLOP/s (a large product of the library: 1080).  fp32, 8 of 2048, 8 heads: 240 / 360 / 510 / 780 us, 143 / 191 / 202 / 176 TFLOP/s (the
+// library's fp32 product: 153).  One query a shape is a pass over K and V: 8 shapes of 609323 keys together, 2 heads of 32, bf16: 28 us
+// and 5 to join the splits, 4.7 TB/s.
 template <typename E, int D, int QW, bool VEC>
 __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::AT_ONCE_FWD)) void attn_fwd_kernel(Args a)
 {
@@ -842,7 +849,11 @@ template <int DT, int WAVES> __device__ __forceinline__ void join_waves(char *ld
         }
 }
 
-// dQ, and D for the pass over the keys: the walk of the forward kernel.
+// dQ, and D for the pass over the keys: the walk of the forward kernel.  D comes from O as it was stored (in bf16 that moves dQ by 2e-4 of
+// its size); dS is rounded to bf16 where the product with K takes it, which together with dQ's own rounding makes 2.4e-3 in bf16.  Two parts of dS
+// would take that back to 1.7e-3 for a third more products.
+// Bound by the matrix pipes (busy 0.60 of the time at 64 channels): bf16, 16 shapes of 4096, 16 heads of 32 / 64 / 96 / 128: 970 / 1520 / 2240 / 3030
+// us, 850 / 1085 / 1100 / 1090 TFLOP/s; fp32, 8 of 2048, 8 heads: 311 / 501 / 830 / 1132 us, 166 / 206 / 187 / 182 TFLOP/s.
 template <typename E, int D, int QW, bool VEC> __device__ __forceinline__ void bwd_dq(const Args &a, int id, char *lds)
 {
     typedef Keys<E, D, QW, VEC> S;
@@ -977,7 +988,10 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
 
 // dK and dV: a wavefront has 32 keys, the queries of all heads that share their head stream past, one head after
 // the other, so the sum over them is taken in registers in a fixed order.  KW wavefronts have keys of their own (4, wide)
-// or all share 32 keys and deal the queries of a tile among them (1, narrow).
+// or all share 32 keys and deal the queries of a tile among them (1, narrow).  p and dS are rounded to bf16 for the products, as above.
+// Bound by the matrix pipes and, with one or two wavefronts a SIMD (a key's two sums and two operands fill the registers), by the steps' own
+// latencies: busy 0.54 of the time at 64 channels.  bf16, 16 shapes of 4096, 16 heads of 32 / 64 / 96 / 128: 1250 / 2320 / 3150 / 5500 us, 880 / 945 / 1045 / 800
+// TFLOP/s; fp32, 8 of 2048, 8 heads: 400 / 715 / 1036 / 1370 us, 172 / 192 / 199 / 201 TFLOP/s.
 template <typename E, int D, int KW, bool VEC> struct Queries {
     static constexpr int WAVES = 4, THREADS = 64 * WAVES, DW = KW == 1 && E::PLANES == 3 && D > 64 ? 2 : 1, QW = WAVES / KW / DW, BK = 32 * KW;
     static constexpr int DT = D / 32 / DW;
@@ -1110,7 +1124,8 @@ __global__ __launch_bounds__((Queries<E, D, KW, VEC>::THREADS), (Queries<E, D, K
     bwd_dkv<E, D, KW, VEC>(a, blockIdx.x, lds);
 }
 
-// Both passes in one launch, for calls neither of which fills the compute units: the first `q_grid` workgroups form dQ, the others dK
+// Both passes in one launch, for calls neither of which fills the compute units (8 shapes of 2381 rows together, 8 heads of 32, fp32: 48 -> 40 us and 5
+// for D; one of 665, 4 of 64, bf16: 26 -> 17 in all): the first `q_grid` workgroups form dQ, the others dK
 // and dV, from a D that attn_delta_kernel left.
 template <typename E, int D, int W> struct Both {
     typedef Keys<E, D, W, true> K;

@@ -3,7 +3,11 @@
 //   backward  h = (x - mu) rs;  w = dy gamma;  dx = rs (w - mean(w) - h mean(w h)) + ds
 //             dgamma = sum over rows of dy h;  dbeta = sum over rows of dy
 // A row is held by LPR lanes, NV vectors of W channels each, and read once: mean and variance come from the
-// registers (two passes over them, so a row with a large mean loses nothing), all sums in fp32.
+// registers (two passes over them, so a row with a large mean loses nothing), all sums in fp32.  LPR is the least number of lanes that holds the row
+// in pieces of up to 16 bytes, so that short rows share a wavefront and no lane idles.  Bound by memory: 609323 rows of 64, fp32 with a
+// residual sum, to bf16: 101 us, 5.4 TB/s (a copy of 2 GB: 4.9); backward of 279722 rows of 128, bf16, with a residual's gradient: 51 to 58 us, 4.9 to
+// 5.6 TB/s; 752 rows of 64 take 3 us, a launch.  Sums over the rows (dgamma, dbeta) are taken by workgroup and added up by a second launch in a
+// fixed order, not by atomics, whose order would change the bits from run to run.
 #pragma once
 #include <hip/hip_runtime.h>
 
