@@ -97,6 +97,11 @@ def load_library():
     if not os.path.exists(_LIBPATH):
         raise ImportError(f"{_LIBPATH} is missing: run `python -c 'import __graft_entry__ as g; "
                           "g.build()'` (hipcc --offload-arch=gfx950) first; there is no fallback")
+    # torch brings a HIP runtime of its own: whichever comes first serves both, and a process with two finds no GPU
+    try:
+        import torch  # noqa: F401
+    except ImportError:
+        pass                                # the host entries need none
     L = C.CDLL(_LIBPATH)
     vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
     L.hch_last_error.restype = C.c_char_p

@@ -1,6 +1,9 @@
 """Refusals of the attention block's C entries, without a GPU: what is wrong is reported before anything is launched.
 Addresses are never read."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -96,3 +99,12 @@ def test_rope_refuses():
     assert f(n=0) == 0
     assert L.hch_rope_bwd(0, P, 64, 0, P, 64, None, 4, 2, 2, 32, (C.c_int32 * 3)(1, 1, 1), 1e4, 1.0, None) == 1
     assert b"hch_rope_bwd" in L.hch_last_error()
+
+
+def test_one_hip_runtime_whichever_is_imported_first():
+    """torch ships a HIP runtime; with the library's loaded beside it neither would work."""
+    code = ("import paper_1803_11385_amd, torch\n"
+            "print(len({l.split()[-1] for l in open('/proc/self/maps') if 'libamdhip64' in l}))")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300, check=True)
+    assert out.stdout.split()[-1] == "1", out.stdout
