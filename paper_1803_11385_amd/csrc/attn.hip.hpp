@@ -849,9 +849,11 @@ template <int DT, int WAVES> __device__ __forceinline__ void join_waves(char *ld
         }
 }
 
-// dQ, and D for the pass over the keys: the walk of the forward kernel.  D comes from O as it was stored (in bf16 that moves dQ by 2e-4 of
-// its size); dS is rounded to bf16 where the product with K takes it, which together with dQ's own rounding makes 2.4e-3 in bf16.  Two parts of dS
-// would take that back to 1.7e-3 for a third more products.
+// dQ, and D for the pass over the keys: the walk of the forward kernel.  dS is rounded to bf16 where the product with K takes it,
+// which together with dQ's own rounding makes 2.4e-3 of its size in bf16; two parts of dS would take that back to 1.7e-3 for a third more
+// products.  D comes from O as it was stored, rounded: 2e-4 of dQ's size where a row's weight is spread over many keys, 2e-3 where a few keys
+// have most of it (3.3e-3 in all).  Without that it would be the sum of p dP over the keys, known when they have all gone past, and what is
+// then to be taken off, the sum of p k, as many products more again as dS k.
 // Bound by the matrix pipes (busy 0.60 of the time at 64 channels): bf16, 16 shapes of 4096, 16 heads of 32 / 64 / 96 / 128: 970 / 1520 / 2240 / 3030
 // us, 850 / 1085 / 1100 / 1090 TFLOP/s; fp32, 8 of 2048, 8 heads: 311 / 501 / 830 / 1132 us, 166 / 206 / 187 / 182 TFLOP/s.
 template <typename E, int D, int QW, bool VEC> __device__ __forceinline__ void bwd_dq(const Args &a, int id, char *lds)
