@@ -37,24 +37,35 @@ int bwd_blocks(int64_t n, int c)
 }
 
 template <int N> using Int = std::integral_constant<int, N>;
-template <typename F> void with_row_shape(int c, bool wide, bool vec, F &&f)
+// run: neighbours that a lane reads at once: 8 (16 bytes of bf16), 4, 2 or 1
+template <typename F> void with_row_shape(int c, int run, F &&f)
 {
-    const RowShape s = row_shape(c, wide ? 8 : 4);
-#define HCH_SHAPE(L, W, V) if (s.lpr == L && s.nv == V) return vec ? f(Int<L>{}, Int<W>{}, Int<V>{}, std::true_type{}) : f(Int<L>{}, Int<W>{}, Int<V>{}, std::false_type{});
-#define HCH_WIDE(L, V) if (s.lpr == L && s.nv == V) return f(Int<L>{}, Int<8>{}, Int<V>{}, std::true_type{});
-    if (wide) { HCH_WIDE(4, 1) HCH_WIDE(8, 1) HCH_WIDE(16, 1) HCH_WIDE(32, 1) HCH_WIDE(64, 1) HCH_WIDE(64, 2) }
-    HCH_SHAPE(4, 4, 1) HCH_SHAPE(8, 4, 1) HCH_SHAPE(16, 4, 1) HCH_SHAPE(32, 4, 1) HCH_SHAPE(64, 4, 1) HCH_SHAPE(64, 4, 2) HCH_SHAPE(64, 4, 4)
-    HCH_SHAPE(256, 4, 2) HCH_SHAPE(256, 4, 4) HCH_SHAPE(256, 4, 8)
+    const RowShape s = row_shape(c, run == 8 ? 8 : 4);
+#define HCH_SHAPE(L, V) if (s.lpr == L && s.nv == V) return run == 4 ? f(Int<L>{}, Int<4>{}, Int<V>{}, Int<4>{}) : run == 2 ? f(Int<L>{}, Int<4>{}, Int<V>{}, Int<2>{}) : f(Int<L>{}, Int<4>{}, Int<V>{}, Int<1>{});
+#define HCH_WIDE(L, V) if (s.lpr == L && s.nv == V) return f(Int<L>{}, Int<8>{}, Int<V>{}, Int<8>{});
+    if (run == 8) { HCH_WIDE(4, 1) HCH_WIDE(8, 1) HCH_WIDE(16, 1) HCH_WIDE(32, 1) HCH_WIDE(64, 1) HCH_WIDE(64, 2) }
+    HCH_SHAPE(4, 1) HCH_SHAPE(8, 1) HCH_SHAPE(16, 1) HCH_SHAPE(32, 1) HCH_SHAPE(64, 1) HCH_SHAPE(64, 2) HCH_SHAPE(64, 4)
+    HCH_SHAPE(256, 2) HCH_SHAPE(256, 4) HCH_SHAPE(256, 8)
 #undef HCH_WIDE
 #undef HCH_SHAPE
 }
+struct Tensor { const void *p; int bytes; };            // of an element
+int run_of(int c, bool wide, std::initializer_list<Tensor> tensors)
+{
+    for (int run = wide && c <= 1024 ? 8 : 4; run > 1; run /= 2) {
+        bool whole = c % run == 0;
+        for (const Tensor &t : tensors) whole = whole && aligned(t.p, std::min(16, run * t.bytes));
+        if (whole) return run;
+    }
+    return 1;
+}
 
-// id of an instance's name, as a profiler prints it: types, then numbers, then a truth value
-template <typename TX, typename TY> int instance_id(const char *kernel, std::initializer_list<int> numbers, bool vec)
+// id of an instance's name, as a profiler prints it: types, numbers, and what is behind them
+template <typename TX, typename TY> int instance_id(const char *kernel, std::initializer_list<int> numbers, const char *end = ">")
 {
     std::string name = std::string(kernel) + "<" + (sizeof(TX) == 4 ? "float" : "__bf16") + ", " + (sizeof(TY) == 4 ? "float" : "__bf16");
     for (int i : numbers) name += ", " + std::to_string(i);
-    return hch::Profiler::get().id_for(name + (vec ? ", true>" : ", false>"));
+    return hch::Profiler::get().id_for(name + end);
 }
 
 template <typename F> void with_types(hch_dtype a, hch_dtype b, F &&f)
@@ -75,18 +86,15 @@ try {
     if (n < 0 || c <= 0 || !(eps >= 0.f)) return fail(HCH_EINVAL, "hch_layernorm_fwd: bad size or eps");
     if (c > MAX_CHANNELS) return fail(HCH_EUNSUPPORTED, "hch_layernorm_fwd: more than 8192 channels");
     if (n == 0) return HCH_OK;
-    const bool vec = c % 4 == 0 && aligned(X, 4 * size_of(x_dtype)) && aligned(R, 4 * size_of(x_dtype)) && aligned(S, 4 * size_of(x_dtype)) &&
-                     aligned(Y, 4 * size_of(y_dtype)) && aligned(gamma, 16) && aligned(beta, 16);
-    const bool wide = vec && (x_dtype == HCH_BF16 || y_dtype == HCH_BF16) && c % 8 == 0 && c <= 1024 && aligned(X, 16) && aligned(R, 16) &&
-                      aligned(S, 16) && aligned(Y, 16);
-    const int groups = hch::norm::THREADS / row_shape(c, wide ? 8 : 4).lpr;
+    const int sx = size_of(x_dtype), run = run_of(c, x_dtype == HCH_BF16 || y_dtype == HCH_BF16, {{X, sx}, {R, sx}, {S, sx}, {Y, size_of(y_dtype)}, {gamma, 4}, {beta, 4}});
+    const int groups = hch::norm::THREADS / row_shape(c, run == 8 ? 8 : 4).lpr;
     const unsigned grid = (unsigned)std::min<int64_t>((n + groups - 1) / groups, 4096);
     {
         with_types(x_dtype, y_dtype, [&](auto tx, auto ty) {
             using TX = decltype(tx);
             using TY = decltype(ty);
-            with_row_shape(c, wide, vec, [&](auto l, auto w, auto v, auto b) {
-                static const int id = instance_id<TX, TY>("norm::layernorm_fwd_kernel", {decltype(l)::value, decltype(w)::value, decltype(v)::value}, decltype(b)::value);
+            with_row_shape(c, run, [&](auto l, auto w, auto v, auto b) {
+                static const int id = instance_id<TX, TY>("norm::layernorm_fwd_kernel", {decltype(l)::value, decltype(w)::value, decltype(v)::value, decltype(b)::value});
                 hch::LaunchTimer lt(id, (hipStream_t)stream, (double)n * c * (size_of(x_dtype) * (R ? 3 : 1) + size_of(y_dtype)), 8.0 * n * c);
                 constexpr auto kernel = hch::norm::layernorm_fwd_kernel<TX, TY, decltype(l)::value, decltype(w)::value, decltype(v)::value, decltype(b)::value>;
                 HCH_LAUNCH(kernel, dim3(grid), dim3(hch::norm::THREADS), 0, (hipStream_t)stream, (const TX *)X, (const TX *)R, (TX *)S,
@@ -122,17 +130,14 @@ try {
     }
     float *part = dgamma ? (float *)workspace : nullptr;
     if (n) {
-        const bool vec = c % 4 == 0 && aligned(X, 4 * size_of(x_dtype)) && aligned(dS, 4 * size_of(x_dtype)) && aligned(dX, 4 * size_of(x_dtype)) &&
-                         aligned(dY, 4 * size_of(dy_dtype)) && aligned(gamma, 16);
         // (fp32 rows with a bf16 gradient are faster by 4 channels: 47 against 50 us at 100000 rows of 256)
-        const bool wide = vec && x_dtype == HCH_BF16 && c % 8 == 0 && c <= 1024 && aligned(X, 16) && aligned(dS, 16) && aligned(dX, 16) &&
-                          aligned(dY, 16);
+        const int sx = size_of(x_dtype), run = run_of(c, x_dtype == HCH_BF16, {{X, sx}, {dS, sx}, {dX, sx}, {dY, size_of(dy_dtype)}, {gamma, 4}});
         {
             with_types(x_dtype, dy_dtype, [&](auto tx, auto ty) {
                 using TX = decltype(tx);
                 using TY = decltype(ty);
-                with_row_shape(c, wide, vec, [&](auto l, auto w, auto v, auto b) {
-                    static const int id = instance_id<TX, TY>("norm::layernorm_bwd_kernel", {decltype(l)::value, decltype(w)::value, decltype(v)::value}, decltype(b)::value);
+                with_row_shape(c, run, [&](auto l, auto w, auto v, auto b) {
+                    static const int id = instance_id<TX, TY>("norm::layernorm_bwd_kernel", {decltype(l)::value, decltype(w)::value, decltype(v)::value, decltype(b)::value});
                     hch::LaunchTimer lt(id, (hipStream_t)stream, (double)n * c * (size_of(x_dtype) * (dS ? 3 : 2) + size_of(dy_dtype)) + 8.0 * n, 14.0 * n * c);
                     constexpr auto kernel = hch::norm::layernorm_bwd_kernel<TX, TY, decltype(l)::value, decltype(w)::value, decltype(v)::value, decltype(b)::value>;
                     HCH_LAUNCH(kernel, dim3(blocks), dim3(hch::norm::THREADS), 0, (hipStream_t)stream, (const TX *)X, stats, gamma,
@@ -200,7 +205,7 @@ hch_status rope(const char *who, double sign, hch_dtype x_dtype, const void *X, 
             using TX = decltype(tx);
             using TY = decltype(ty);
             auto launch = [&](auto k, auto v) {
-                static const int id = instance_id<TX, TY>("rope::rope_kernel", {decltype(k)::value}, decltype(v)::value);
+                static const int id = instance_id<TX, TY>("rope::rope_kernel", {decltype(k)::value}, decltype(v)::value ? ", true>" : ", false>");
                 hch::LaunchTimer lt(id, (hipStream_t)stream, (double)n * heads * head_dim * (sx + sy) + 12.0 * n, 6.0 * n * rot_heads * pairs);
                 constexpr auto kernel = hch::rope::rope_kernel<TX, TY, decltype(k)::value, decltype(v)::value>;
                 HCH_LAUNCH(kernel, dim3((unsigned)blocks, (unsigned)((pieces + hch::rope::THREADS - 1) / hch::rope::THREADS)), dim3(hch::rope::THREADS),
