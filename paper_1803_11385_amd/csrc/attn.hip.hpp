@@ -538,8 +538,8 @@ template <typename E, int D, int QW, bool VEC> struct Keys {
 // Bound by the matrix pipes and the softmax between the products: at 64 channels the pipes work 0.45 of the time, at 128 0.56, and the vector
 // units most of the rest.  bf16, 16 shapes of 4096, 16 heads of 32 / 64 / 96 / 128 channels: 947 / 1225 / 1630 / 2100 us, 580 / 900 / 1010 /
 // 1050 TFLOP/s (a large product of the library: 1080).  fp32, 8 of 2048, 8 heads: 240 / 360 / 510 / 780 us, 143 / 191 / 202 / 176 TFLOP/s (the
-// library's fp32 product: 153).  One query a shape is a pass over K and V: 8 shapes of 609323 keys together, 2 heads of 32, bf16: 28 us
-// and 5 to join the splits, 4.7 TB/s.
+// library's fp32 product: 153).  One query a shape is a pass over K and V: 8 shapes of 609323 keys together, 2 heads of 32, bf16: 37 us
+// from memory (4.2 TB/s; 28 where the last-level cache still has them) and 5.5 to join the splits.
 template <typename E, int D, int QW, bool VEC>
 __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC>::AT_ONCE_FWD)) void attn_fwd_kernel(Args a)
 {
