@@ -545,7 +545,7 @@ hch_status hch_layernorm_bwd(hch_dtype x_dtype, const void *X, const float *stat
  * hch_rope_bwd takes the gradient back through it (turns by -t).
  * Errors: HCH_EINVAL (null pointer, head_dim odd, sizes negative, sections beyond head_dim / 2 pairs, strides
  * below heads * head_dim, base <= 0, base or scale not finite, unknown dtype), HCH_EUNSUPPORTED (head_dim > 256,
- * more than 2^31 workgroups), HCH_EHIP.
+ * heads * head_dim > 2^22, more than 2^31 workgroups), HCH_EHIP.
  */
 hch_status hch_rope_fwd(hch_dtype x_dtype, const void *X, int64_t ld_x, hch_dtype y_dtype, void *Y, int64_t ld_y,
                         const int32_t *coords, int64_t n, int32_t heads, int32_t rot_heads, int32_t head_dim,

@@ -189,6 +189,7 @@ hch_status rope(const char *who, double sign, hch_dtype x_dtype, const void *X, 
     if (!coords && rot_heads && pairs) return fail(HCH_EINVAL, name + ": coords is null");
     if (X == Y && (x_dtype != y_dtype || ld_x != ld_y)) return fail(HCH_EINVAL, name + ": in place needs one type and one row stride");
     if (n == 0) return HCH_OK;
+    if ((int64_t)heads * head_dim > (1 << 22)) return fail(HCH_EUNSUPPORTED, name + ": more than 2^22 elements in a row");
     const int sx = size_of(x_dtype), sy = size_of(y_dtype);
     const bool vec = head_dim % 4 == 0 && ld_x % 4 == 0 && ld_y % 4 == 0 && aligned(X, 4 * sx) && aligned(Y, 4 * sy);
     const bool eight = vec && x_dtype == HCH_BF16 && head_dim % 8 == 0 && ld_x % 8 == 0 && ld_y % 8 == 0 && aligned(X, 16) && aligned(Y, 16);
@@ -199,7 +200,7 @@ hch_status rope(const char *who, double sign, hch_dtype x_dtype, const void *X, 
     int rows = n >= (int64_t)16384 * step / 8 ? 2 * step : step;
     if (turned) rows = std::min(rows, hch::rope::ENTRIES / turned);
     const int64_t blocks = (n + rows - 1) / rows;
-    if (blocks > 0x7fffffff || (int64_t)heads * head_dim > (1 << 22)) return fail(HCH_EUNSUPPORTED, name + ": too many rows or heads for one launch");
+    if (blocks > 0x7fffffff) return fail(HCH_EUNSUPPORTED, name + ": too many rows for one launch");
     {
         with_types(x_dtype, y_dtype, [&](auto tx, auto ty) {
             using TX = decltype(tx);

@@ -108,3 +108,12 @@ def test_one_hip_runtime_whichever_is_imported_first():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300, check=True)
     assert out.stdout.split()[-1] == "1", out.stdout
+
+
+def test_rope_refuses_rows_whose_length_passes_32_bits():
+    """2^24 heads of 256 channels: the product is 2^32.  In a process of its own, which has to end by itself."""
+    code = ("import ctypes as C\nimport paper_1803_11385_amd as hch\n"
+            "print(hch.load_library().hch_rope_fwd(0, 4096, 1 << 33, 0, 8192, 1 << 33, 4096, 4, 1 << 24, 1, 256, (C.c_int32 * 3)(1, 1, 1), 1e4, 1.0, None))")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and out.stdout.split()[-1] == "5", (out.returncode, out.stdout, out.stderr[-300:])
