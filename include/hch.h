@@ -520,8 +520,9 @@ hch_status hch_relu_bwd(const float *y, const float *dy, float *dx, int64_t n, v
  *                                             reaches s on the residual path) may be NULL; dX may be dS
  *   dgamma, dbeta  DEVICE [c] float, overwritten; both NULL: not computed, and no workspace needed
  *   workspace      DEVICE, 256-byte aligned, hch_layernorm_workspace_bytes(n, c) bytes (0 on bad arguments)
- * n = 0 is allowed (dgamma = dbeta = 0).  Errors: HCH_EINVAL (null pointer, one of a pair alone, n < 0, c <= 0, eps
- * negative or NaN, unknown dtype, workspace misaligned), HCH_EUNSUPPORTED (c > 8192), HCH_EWORKSPACE, HCH_EHIP.
+ * n = 0 is allowed, with null pointers for what has no rows (dgamma = dbeta = 0).  Errors: HCH_EINVAL (null
+ * pointer, one of a pair alone, n < 0, c <= 0, eps negative or NaN, unknown dtype, workspace misaligned),
+ * HCH_EUNSUPPORTED (c > 8192), HCH_EWORKSPACE, HCH_EHIP.
  */
 hch_status hch_layernorm_fwd(hch_dtype x_dtype, const void *X, const void *R, void *S, const float *gamma,
                              const float *beta, hch_dtype y_dtype, void *Y, float *stats, int64_t n, int32_t c,
@@ -542,7 +543,7 @@ hch_status hch_layernorm_bwd(hch_dtype x_dtype, const void *X, const float *stat
  *           allowed with one type and one stride
  *   coords  DEVICE [n][3] int32 (hch_level_desc.coords is one); may be NULL if nothing turns
  *   sections  HOST [3]
- * hch_rope_bwd takes the gradient back through it (turns by -t).
+ * hch_rope_bwd takes the gradient back through it (turns by -t).  n = 0 is allowed, as above.
  * Errors: HCH_EINVAL (null pointer, head_dim odd, sizes negative, sections beyond head_dim / 2 pairs, strides
  * below heads * head_dim, base <= 0, base or scale not finite, unknown dtype), HCH_EUNSUPPORTED (head_dim > 256,
  * heads * head_dim > 2^22, more than 2^31 workgroups), HCH_EHIP.

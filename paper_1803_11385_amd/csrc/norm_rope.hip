@@ -82,7 +82,7 @@ extern "C" hch_status hch_layernorm_fwd(hch_dtype x_dtype, const void *X, const 
                                         hch_dtype y_dtype, void *Y, float *stats, int64_t n, int32_t c, float eps, void *stream)
 try {
     if (!known(x_dtype) || !known(y_dtype)) return fail(HCH_EINVAL, "hch_layernorm_fwd: unknown dtype");
-    if (!X || !Y || (R != nullptr) != (S != nullptr)) return fail(HCH_EINVAL, "hch_layernorm_fwd: null pointer, or only one of R and S");
+    if ((n && (!X || !Y)) || (R != nullptr) != (S != nullptr)) return fail(HCH_EINVAL, "hch_layernorm_fwd: null pointer, or only one of R and S");
     if (n < 0 || c <= 0 || !(eps >= 0.f)) return fail(HCH_EINVAL, "hch_layernorm_fwd: bad size or eps");
     if (c > MAX_CHANNELS) return fail(HCH_EUNSUPPORTED, "hch_layernorm_fwd: more than 8192 channels");
     if (n == 0) return HCH_OK;
@@ -119,7 +119,7 @@ extern "C" hch_status hch_layernorm_bwd(hch_dtype x_dtype, const void *X, const 
                                         void *workspace, size_t ws_bytes, void *stream)
 try {
     if (!known(x_dtype) || !known(dy_dtype)) return fail(HCH_EINVAL, "hch_layernorm_bwd: unknown dtype");
-    if (!X || !stats || !dY || !dX || (dgamma != nullptr) != (dbeta != nullptr))
+    if ((n && (!X || !stats || !dY || !dX)) || (dgamma != nullptr) != (dbeta != nullptr))
         return fail(HCH_EINVAL, "hch_layernorm_bwd: null pointer, or only one of dgamma and dbeta");
     if (n < 0 || c <= 0) return fail(HCH_EINVAL, "hch_layernorm_bwd: bad size");
     if (c > MAX_CHANNELS) return fail(HCH_EUNSUPPORTED, "hch_layernorm_bwd: more than 8192 channels");
@@ -172,7 +172,7 @@ hch_status rope(const char *who, double sign, hch_dtype x_dtype, const void *X, 
 {
     const std::string name = who;
     if (!known(x_dtype) || !known(y_dtype)) return fail(HCH_EINVAL, name + ": unknown dtype");
-    if (!X || !Y || !sections) return fail(HCH_EINVAL, name + ": null pointer");
+    if ((n && (!X || !Y)) || !sections) return fail(HCH_EINVAL, name + ": null pointer");
     if (n < 0 || heads <= 0 || rot_heads < 0 || rot_heads > heads || head_dim <= 0 || head_dim % 2) return fail(HCH_EINVAL, name + ": bad size");
     if (head_dim > 2 * hch::rope::MAX_PAIRS) return fail(HCH_EUNSUPPORTED, name + ": more than 256 channels per head");
     if (ld_x < (int64_t)heads * head_dim || ld_y < (int64_t)heads * head_dim) return fail(HCH_EINVAL, name + ": row stride below heads * head_dim");
@@ -186,8 +186,8 @@ hch_status rope(const char *who, double sign, hch_dtype x_dtype, const void *X, 
             table.axis[pairs] = (uint8_t)a;
         }
     }
-    if (!coords && rot_heads && pairs) return fail(HCH_EINVAL, name + ": coords is null");
-    if (X == Y && (x_dtype != y_dtype || ld_x != ld_y)) return fail(HCH_EINVAL, name + ": in place needs one type and one row stride");
+    if (n && !coords && rot_heads && pairs) return fail(HCH_EINVAL, name + ": coords is null");
+    if (n && X == Y && (x_dtype != y_dtype || ld_x != ld_y)) return fail(HCH_EINVAL, name + ": in place needs one type and one row stride");
     if (n == 0) return HCH_OK;
     if ((int64_t)heads * head_dim > (1 << 22)) return fail(HCH_EUNSUPPORTED, name + ": more than 2^22 elements in a row");
     const int sx = size_of(x_dtype), sy = size_of(y_dtype);

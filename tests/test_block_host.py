@@ -117,3 +117,17 @@ def test_rope_refuses_rows_whose_length_passes_32_bits():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert out.returncode == 0 and out.stdout.split()[-1] == "5", (out.returncode, out.stdout, out.stderr[-300:])
+
+
+def test_no_rows_need_no_tensors():
+    """The address of a tensor without elements is null: with n = 0 that is no error in any of the entries."""
+    L = hch.load_library()
+    assert L.hch_layernorm_fwd(0, None, None, None, None, None, 0, None, None, 0, 8, 1e-5, None) == 0
+    assert L.hch_layernorm_bwd(0, None, None, None, 0, None, None, None, None, None, 0, 8, None, 0, None) == 0
+    for f in (L.hch_rope_fwd, L.hch_rope_bwd):
+        assert f(0, None, 64, 1, None, 64, None, 0, 2, 2, 32, (C.c_int32 * 3)(1, 1, 1), 1e4, 1.0, None) == 0
+    # what does not depend on the rows is still looked at
+    assert L.hch_layernorm_fwd(0, None, None, None, None, None, 0, None, None, 0, 0, 1e-5, None) == 1
+    assert L.hch_layernorm_fwd(0, None, P, None, None, None, 0, None, None, 0, 8, 1e-5, None) == 1
+    assert L.hch_layernorm_bwd(0, None, None, None, 0, None, None, None, P, None, 0, 8, P, 1 << 20, None) == 1
+    assert L.hch_rope_fwd(0, None, 64, 1, None, 64, None, 0, 2, 2, 32, None, 1e4, 1.0, None) == 1

@@ -218,3 +218,20 @@ def test_refusals():
     assert status(rope, F, X, F, Y, p, 4, 1, 1, 8, (1, 1, 1), 10.0, float("nan")) == 1
     w = torch.zeros((4, 258), device="cuda")
     assert status(rope, F, w, F, w.clone(), p, 4, 1, 1, 258, (1, 1, 1)) == 5
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_tensors_without_rows(x):
+    code, t = TYPES[x]
+    e, p = torch.empty((0, 24), dtype=t, device="cuda"), torch.empty((0, 3), dtype=torch.int32, device="cuda")
+    stats = torch.empty((0, 2), device="cuda")
+    hch.hch_layernorm_fwd(code, e, None, None, None, None, code, e, stats, 0, 24)
+    # S of no rows has no address either: R and S are a pair as long as both are given or both are not
+    hch.hch_layernorm_fwd(code, e, e, e, None, None, code, e, stats, 0, 24)
+    dg, db = torch.ones(24, device="cuda"), torch.ones(24, device="cuda")
+    hch.hch_layernorm_bwd(code, e, stats, None, code, e, None, e, dg, db, 0, 24, _ws(hch.hch_layernorm_workspace_bytes(0, 24)))
+    hch.hch_layernorm_bwd(code, e, stats, None, code, e, e, e, None, None, 0, 24, None)
+    for f in (hch.hch_rope_fwd, hch.hch_rope_bwd):
+        f(code, e, code, torch.empty_like(e), p, 0, 3, 2, 8, (1, 1, 1))
+    torch.cuda.synchronize()
+    assert not dg.any() and not db.any()
