@@ -546,7 +546,7 @@ hch_status hch_layernorm_bwd(hch_dtype x_dtype, const void *X, const float *stat
  * hch_rope_bwd takes the gradient back through it (turns by -t).  n = 0 is allowed, as above.
  * Errors: HCH_EINVAL (null pointer, head_dim odd, sizes negative, sections beyond head_dim / 2 pairs, strides
  * below heads * head_dim, base <= 0, base or scale not finite, unknown dtype), HCH_EUNSUPPORTED (head_dim > 256,
- * heads * head_dim > 2^22, more than 2^31 workgroups), HCH_EHIP.
+ * heads * head_dim > 2^22, more than 2^24 - 1 workgroups: at least 2^27 rows), HCH_EHIP.
  */
 hch_status hch_rope_fwd(hch_dtype x_dtype, const void *X, int64_t ld_x, hch_dtype y_dtype, void *Y, int64_t ld_y,
                         const int32_t *coords, int64_t n, int32_t heads, int32_t rot_heads, int32_t head_dim,
@@ -580,8 +580,8 @@ hch_status hch_rope_bwd(hch_dtype dy_dtype, const void *dY, int64_t ld_dy, hch_d
  * Any head_dim from 1 to 128; multiples of 16 bytes in head_dim, strides and addresses are faster.
  * Errors: HCH_EINVAL (null pointer, negative size, heads_q not a multiple of heads_kv, scale not positive and
  * finite, strides below a row's length, unknown dtype, workspace misaligned), HCH_EUNSUPPORTED (head_dim > 128,
- * strides of 2^22 elements or more, 2^15 heads or more, n_q * heads_q or n_k of 2^31 - 256 or more), HCH_EWORKSPACE,
- * HCH_EHIP.
+ * strides of 2^22 elements or more, 2^15 heads or more, n_q * heads_q or n_k of 2^31 - 256 or more, more than 2^24 - 1
+ * workgroups: one for each key head and tile of 128 rows (of 32 where shapes are short) and one more a shape), HCH_EWORKSPACE, HCH_EHIP.
  */
 typedef struct {
     hch_dtype dtype;

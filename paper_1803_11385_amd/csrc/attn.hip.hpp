@@ -208,14 +208,25 @@ __device__ __forceinline__ constexpr int reg_row(int r) { return 8 * (r >> 2) + 
 // neighbours of a head are kept on one XCD: they read the same keys, from its L2.  With few, one by one (512 of
 // dQ, 8 shapes of 2000 rows, 32 channels, fp32: 108 us in runs of 16, 81 so), and all heads of a tile on one XCD, since they share
 // lines of memory (8 shapes of 76165 keys, 2 heads of 32, bf16, one query: 47 us apart, 27 together).
+struct WorkShape { int run; int64_t per_head, grid; };
+inline WorkShape work_shape(int64_t slots, int splits, int heads)
+{
+    const int64_t each = slots * splits, total = each * heads;
+    WorkShape w;
+    w.run = total >= 4096 ? 16 : total >= 1024 ? 4 : 1;
+    const int whole = w.run == 1 ? 8 : w.run;
+    w.per_head = (each + whole - 1) / whole * whole;
+    w.grid = (w.per_head * heads + 8 * w.run - 1) / (8 * w.run) * (8 * w.run);
+    return w;
+}
+constexpr int64_t MAX_GRID = 0xffffffffll / 256;         // a launch's work items are counted in 32 bits
 inline void set_work(Args &a)
 {
-    const int64_t each = (int64_t)a.slots * a.splits, total = each * a.hkv;
-    a.run = total >= 4096 ? 16 : total >= 1024 ? 4 : 1;
-    const int whole = a.run == 1 ? 8 : a.run;
-    a.per_head = (int)((each + whole - 1) / whole * whole);
+    const WorkShape w = work_shape(a.slots, a.splits, a.hkv);
+    a.run = w.run;
+    a.per_head = (int)w.per_head;
 }
-inline unsigned work_grid(const Args &a) { return (unsigned)(((int64_t)a.per_head * a.hkv + 8 * a.run - 1) / (8 * a.run) * (8 * a.run)); }
+inline unsigned work_grid(const Args &a) { return (unsigned)work_shape(a.slots, a.splits, a.hkv).grid; }
 struct Work { int head, slot, split; };         // slot beyond the last: nothing to do
 __device__ __forceinline__ Work work_of(const Args &a, int id)
 {

@@ -135,7 +135,7 @@ hch_status check_sizes(const char *who, const hch_attn_desc *p)
     if (p->batch == 0 && (p->n_q || p->n_k)) return no(HCH_EINVAL, ": rows without a shape");
     return HCH_OK;
 }
-bool launchable(const hch_attn_desc &p, const Plan &r) { return r.slots * r.splits <= 0x7fffffff / p.heads_kv - 256; }
+bool launchable(const hch_attn_desc &p, const Plan &r) { return hch::attn::work_shape(r.slots, r.splits, p.heads_kv).grid <= hch::attn::MAX_GRID; }
 
 hch_status check_call(const char *who, const hch_attn_desc *p, const void *workspace, size_t ws_bytes, size_t need)
 {
@@ -199,7 +199,7 @@ try {
     st = check_call("hch_attn_fwd", desc, workspace, ws_bytes, fwd_bytes(p, r));
     if (st != HCH_OK) return st;
     if ((p.n_q && (!Q || !O)) || (p.n_k && (!K || !V))) return fail(HCH_EINVAL, "hch_attn_fwd: null pointer");
-    if (!launchable(p, r)) return fail(HCH_EUNSUPPORTED, "hch_attn_fwd: too many rows for one launch");
+    if (!launchable(p, r)) return fail(HCH_EUNSUPPORTED, "hch_attn_fwd: more than 2^24 - 1 workgroups in a launch");
     if (!p.n_q) return HCH_OK;
     Args a = args_of(p);
     a.Q = Q; a.K = K; a.V = V; a.Ow = O; a.lse = lse;
@@ -228,7 +228,7 @@ try {
     if (p.ld_do < wq || p.ld_dq < wq || p.ld_dk < wk || p.ld_dv < wk) return fail(HCH_EINVAL, "hch_attn_bwd: row stride below a row's length");
     if (std::max({p.ld_do, p.ld_dq, p.ld_dk, p.ld_dv}) >= 1 << 22) return fail(HCH_EUNSUPPORTED, "hch_attn_bwd: row stride of 2^22 elements or more");
     if ((p.n_q && (!Q || !O || !lse || !dO || !dQ)) || (p.n_k && (!K || !V || !dK || !dV))) return fail(HCH_EINVAL, "hch_attn_bwd: null pointer");
-    if (!launchable(p, r.dq) || !launchable(p, r.dkv)) return fail(HCH_EUNSUPPORTED, "hch_attn_bwd: too many rows for one launch");
+    if (!launchable(p, r.dq) || !launchable(p, r.dkv)) return fail(HCH_EUNSUPPORTED, "hch_attn_bwd: more than 2^24 - 1 workgroups in a launch");
     Args a = args_of(p);
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse = const_cast<float *>(lse); a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV;
     a.vec = whole(p, {Q, K, V, O, dO, dQ, dK, dV}, {p.ld_q, p.ld_k, p.ld_v, p.ld_o, p.ld_do, p.ld_dq, p.ld_dk, p.ld_dv});

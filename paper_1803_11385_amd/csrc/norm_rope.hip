@@ -199,8 +199,8 @@ hch_status rope(const char *who, double sign, hch_dtype x_dtype, const void *X, 
     const int turned = rot_heads ? pairs : 0;
     int rows = n >= (int64_t)16384 * step / 8 ? 2 * step : step;
     if (turned) rows = std::min(rows, hch::rope::ENTRIES / turned);
-    const int64_t blocks = (n + rows - 1) / rows;
-    if (blocks > 0x7fffffff) return fail(HCH_EUNSUPPORTED, name + ": too many rows for one launch");
+    const int64_t blocks = (n - 1) / rows + 1;
+    if (blocks > 0xffffffffll / hch::rope::THREADS) return fail(HCH_EUNSUPPORTED, name + ": more than 2^24 - 1 workgroups in a launch");
     {
         with_types(x_dtype, y_dtype, [&](auto tx, auto ty) {
             using TX = decltype(tx);

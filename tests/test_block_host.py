@@ -131,3 +131,20 @@ def test_no_rows_need_no_tensors():
     assert L.hch_layernorm_fwd(0, None, P, None, None, None, 0, None, None, 0, 8, 1e-5, None) == 1
     assert L.hch_layernorm_bwd(0, None, None, None, 0, None, None, None, P, None, 0, 8, P, 1 << 20, None) == 1
     assert L.hch_rope_fwd(0, None, 64, 1, None, 64, None, 0, 2, 2, 32, None, 1e4, 1.0, None) == 1
+
+
+def test_attention_refuses_launches_of_2_to_24_workgroups():
+    """A launch's work items are counted in 32 bits: 2^24 workgroups of 256 are refused before anything is launched.  (Sizes beyond
+    the limit only: others would be launched.)"""
+    one = dict(heads_q=1, heads_kv=1, nbytes=1 << 62)
+    many = dict(heads_q=16, heads_kv=16, nbytes=1 << 62, **{ld: 512 for ld in ("ld_q", "ld_k", "ld_v", "ld_o", "ld_do", "ld_dq", "ld_dk", "ld_dv")})
+    for f in (_fwd, _bwd):
+        assert f(n_q=2 ** 31 - 257, n_k=1 << 20, batch=1 << 23, **one) == 5       # tiles of rows
+        assert f(n_q=1 << 24, n_k=1 << 24, batch=1 << 24, **one) == 5             # shapes of one row
+        assert f(n_q=1 << 20, n_k=1 << 20, batch=1 << 20, **many) == 5            # for each of 16 key heads
+    assert _bwd(n_q=8, n_k=2 ** 31 - 257, batch=8, **many) == 5                   # one pass of the gradient would fit
+
+
+def test_rope_refuses_launches_of_2_to_24_workgroups():
+    f = hch.load_library().hch_rope_fwd
+    assert f(0, P, 1 << 22, 0, 2 * P, 1 << 22, P, 1 << 28, 1 << 14, 1, 256, (C.c_int32 * 3)(1, 1, 1), 1e4, 1.0, None) == 5
