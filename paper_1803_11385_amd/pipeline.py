@@ -130,6 +130,12 @@ class Encoder:
         self.backward()
 
 
+def _by_eights(n, width, dtype, device):
+    """An empty [n][width] tensor, and its memory as rows of 8 elements (a few more than there are)."""
+    t = torch.empty(((n * width + 7) // 8, 8), dtype=dtype, device=device)
+    return t.view(-1)[: n * width].view(n, width), t
+
+
 class AttentionBlock:
     """A pre-norm attention block over the voxels of one level, each shape by itself, forward and backward:
 
@@ -171,10 +177,11 @@ class AttentionBlock:
         self.lse = torch.empty((n, heads_q), **f32)
         # backward; in fp32 the gradients go into products as they are
         same = dtype == B.HCH_F32
-        self.dY, self.dX, self.dS, self.dh = (torch.empty((n, c), **f32) for _ in range(4))
-        self.dP = self.dS if same else torch.empty((n, c), **t)
-        self.dO32 = torch.empty((n, wq), **f32)
-        self.dO = self.dO32 if same else torch.empty((n, wq), **t)
+        self.dY, self.dX, self.dh = (torch.empty((n, c), **f32) for _ in range(3))
+        (self.dS, dS8), (self.dO32, dO32_8) = _by_eights(n, c, **f32), _by_eights(n, wq, **f32)
+        self.dP, dP8 = (self.dS, None) if same else _by_eights(n, c, **t)
+        self.dO, dO8 = (self.dO32, None) if same else _by_eights(n, wq, **t)
+        self._to_products = (dS8, dP8), (dO32_8, dO8)
         self.dqkv = torch.empty((n, self.wide), **t)
         self.dq, self.dk, self.dv = self.dqkv[:, :wq], self.dqkv[:, wq: wq + wk], self.dqkv[:, wq + wk:]
         b = self.offsets.numel() - 1
@@ -184,11 +191,10 @@ class AttentionBlock:
             need += [B.hch_sconv_workspace_bytes(levels, level, 1, 1, ci, co, dtype, kind) for ci, co in ((c, self.wide), (wq, c))]
         self.ws = _aligned_bytes(max(need), device)
 
-    def _convert(self, x, y):
-        """y = x in the products' type: rotary positions that turn nothing."""
-        if y is not x:
-            w = x.shape[1] // 2
-            B.hch_rope_fwd(B.HCH_F32, x, self.dtype, y, None, self.n, w, 0, 2, (0, 0, 0))
+    def _convert(self, x8, y8):
+        """y = x in the products' type, all elements in rows of 8 whatever the width: rotary positions that turn nothing."""
+        if y8 is not None:
+            B.hch_rope_fwd(B.HCH_F32, x8, self.dtype, y8, None, x8.shape[0], 1, 0, 8, (0, 0, 0))
 
     def forward(self):
         """X -> S, Y"""
@@ -208,10 +214,10 @@ class AttentionBlock:
         n, c, wq, dt, lv = self.n, self.c, self.hq * self.d, self.dtype, (self.levels, self.level, 1, 1)
         B.hch_layernorm_bwd(B.HCH_F32, self.S, self.stats[1], self.gamma[1], B.HCH_F32, self.dY, dS, self.dS, self.dgamma[1],
                             self.dbeta[1], n, c, self.ws)
-        self._convert(self.dS, self.dP)
+        self._convert(*self._to_products[0])
         B.hch_sconv_bwd_weight(*lv, dt, self.O, self.dP, self.dWo, self.field, wq, c, self.ws)
         B.hch_sconv_bwd_data(*lv, dt, self.dP, self.Wo, self.dO32, self.field_t, wq, c, self.ws)
-        self._convert(self.dO32, self.dO)
+        self._convert(*self._to_products[1])
         B.hch_attn_bwd(dt, self.q, self.k, self.v, self.O, self.lse, self.dO, self.dq, self.dk, self.dv, self.offsets, self.offsets,
                        self.key_mask, self.hq, self.hkv, self.d, self.scale, self.ws)
         B.hch_rope_bwd(dt, self.dqkv, dt, self.dqkv, self.positions, n, self.hq + 2 * self.hkv, self.hq + self.hkv, self.d,

@@ -78,3 +78,20 @@ def test_block_against_automatic_differentiation(dtype, bar, c, hq, hkv, d, mask
         e = want[name]
         off = (g.double().cpu() - e).abs() / (e.abs() + e.pow(2).mean().sqrt())
         assert off.max() <= bar, f"{name}: {off.max():.2e} of {bar}"
+
+
+@pytest.mark.parametrize("dtype,bar", [(hch.HCH_F32, 1e-4), (hch.HCH_BF16, 2e-2)])
+@pytest.mark.parametrize("c", [33, 47, 34, 36])
+def test_every_channel_count(monkeypatch, dtype, bar, c):
+    """Widths that are multiples of nothing, 2 and 4; every buffer of the block holds NaN before the passes, so that an element that
+    none of them writes shows."""
+    from paper_1803_11385_amd import pipeline
+    init = pipeline.AttentionBlock.__init__
+
+    def poisoned(self, *args, **kw):
+        init(self, *args, **kw)
+        for name in ("S", "Y", "P", "h", "O", "proj", "qkv", "lse", "dX", "dS", "dh", "dP", "dO32", "dO", "dqkv", "dWqkv", "dWo"):
+            getattr(self, name).fill_(float("nan"))
+
+    monkeypatch.setattr(pipeline.AttentionBlock, "__init__", poisoned)
+    test_block_against_automatic_differentiation(dtype, bar, c, 4, 2, 16, True)
