@@ -582,6 +582,7 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
 #pragma unroll
     for (int dt = 0; dt < S::DT; ++dt) acc[dt] = f32x16{};
     float m = -INFINITY, l = 0.f;
+    bool some = false;                                      // a key was seen
 
     // The next tile is on its way while this one is multiplied: in registers, or straight to the other buffer.
     typedef Stage<E, D, S::BK, S::THREADS> Regs;
@@ -609,6 +610,7 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
 #pragma unroll
         for (int i = 0; i < S::WORDS; ++i) {
             keep[i] = __ballot(seen[i] != 0);
+            some |= keep[i] != 0;
             all &= S::BK - 64 * i >= 64 ? keep[i] == ~0ull : (uint32_t)keep[i] == ~0u;
         }
         if constexpr (S::DIRECT) {
@@ -687,6 +689,14 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
         __builtin_amdgcn_s_setprio(0);
     }
     l += other_half(l);
+    // Rows that saw no key are 0 whatever their queries hold: NaN and infinity have met the zeros of keys that are left out, and
+    // made NaN of them.
+    if (!some) {
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < S::DT; ++dt) acc[dt] = f32x16{};
+    }
 
     if constexpr (QW == 1) {                            // the wavefronts' shares of the keys, joined in LDS
         __syncthreads();

@@ -349,3 +349,27 @@ def test_refusals():
     assert hch.hch_attn_workspace_bytes(hch.HCH_WS_FWD, c.code, 1, 4, 6, 2, 3, 32) == 0
     assert hch.hch_attn_workspace_bytes(hch.HCH_WS_FWD, c.code, 0, 4, 6, 2, 2, 32) == 0
     c.run().check()                                             # and a call after them is none the worse
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("d", [24, 64, 96, 128])
+def test_a_row_without_keys_is_zero_whatever_its_query_holds(dtype, pad, d):
+    """All keys of the second shape are left out and its queries hold NaN, infinities and the type's largest numbers: o = 0, lse = -inf
+    and no gradient, in both forms, in whole pieces and not, with split keys and without."""
+    names = set()
+    many = [100 + 7 * (i % 13) for i in range(70)]
+    for lq, lk, hq, hkv in ((many, many, 4, 2), ([4, 3], [40, 50], 4, 2), ([1, 1, 2], [900, 1500, 700], 4, 2), ([300, 200], [200, 300], 4, 2),
+                            ([71, 71], [113, 113], 16, 8), ([57] * 3, [57] * 3, 8, 4), ([1] * 83, [7] * 83, 8, 8), ([89] * 4, [111] * 4, 8, 8),
+                            ([1] * 47, [411] * 47, 4, 4), ([1, 1], [855, 855], 1, 1), ([128, 128], [56, 56], 1, 1), ([3] * 87, [5] * 87, 64, 8)):
+        c = Case(dtype, lq, lk, hq, hkv, d, masked=0.1, pad=pad, junk=True, seed=d + pad)
+        rows = c.t["q"][c.qo[1]: c.qo[2]]
+        for i, x in enumerate((float("nan"), float("inf"), float("-inf"), torch.finfo(c.dt).max)):
+            rows[:, i::5] = x
+        names |= set(_launched(c.run))
+        c.check()
+    engine, whole = {"f32": "Split", "bf16": "Bf16"}[dtype], "false" if pad else "true"
+    narrow = 128 if dtype == "f32" and d > 64 else (d + 31) // 32 * 32
+    for width, form in (((d + 31) // 32 * 32, 4), (narrow, 1)):
+        assert f"attn::attn_fwd_kernel<attn::{engine}, {width}, {form}, {whole}>" in names, sorted(names)
+    assert any("attn_join_kernel" in n for n in names), sorted(names)
