@@ -722,7 +722,7 @@ def _rows(t, what, dtype, n, width):
     ld, step = t.stride()
     if (step != 1 and width > 1) or (n > 1 and ld < width):
         raise HchError(1, f"{what}: the elements of a row must lie side by side and rows must not overlap")
-    return t.data_ptr(), ld if n > 1 else max(ld, width)
+    return t.data_ptr(), ld if n > 1 else width     # nothing lies behind the only row
 
 
 def _rope(name, x_dtype, X, y_dtype, Y, coords, n, heads, rot_heads, head_dim, sections, base, scale, stream):

@@ -373,3 +373,15 @@ def test_a_row_without_keys_is_zero_whatever_its_query_holds(dtype, pad, d):
     for width, form in (((d + 31) // 32 * 32, 4), (narrow, 1)):
         assert f"attn::attn_fwd_kernel<attn::{engine}, {width}, {form}, {whole}>" in names, sorted(names)
     assert any("attn_join_kernel" in n for n in names), sorted(names)
+
+
+def test_one_row_of_any_stride():
+    """What lies behind the only row is never stepped over, however wide its tensor is."""
+    c = Case("f32", [1], [1], 2, 1, 32)
+    wide = torch.zeros((1, 1 << 22), device="cuda")
+    wide[:, :64] = c.t["q"]
+    c.t["q"], c.whole["q"] = wide[:, :64], torch.full((1, 64), float("nan"), device="cuda")
+    t, (hq, hkv, d) = c.t, c.dims
+    hch.hch_attn_fwd(c.code, t["q"], t["k"], t["v"], t["o"], c.lse, c.dqo, c.dko, None, hq, hkv, d, c.scale, c.ws)
+    torch.cuda.synchronize()
+    assert (np.abs(t["o"].double().cpu().numpy() - c.want["o"]) <= c.bounds()["o"]).all()
