@@ -766,9 +766,9 @@ def _attn_desc(dtype, Q, K, q_offsets, k_offsets, key_mask, heads_q, heads_kv, h
     if batch < 0 or k_offsets.numel() != batch + 1:
         raise HchError(1, "q_offsets and k_offsets: batch + 1 entries each")
     if key_mask is not None:
+        mask = _dp(key_mask, "key_mask", None, n_k)
         if key_mask.element_size() != 1:
             raise HchError(1, "key_mask: must have elements of one byte")
-        mask = _dp(key_mask, "key_mask", None, n_k)
     return _AttnDesc(dt, batch, heads_q, heads_kv, head_dim, scale, n_q, n_k, qo, ko, mask), heads_q * head_dim, heads_kv * head_dim
 
 

@@ -385,3 +385,10 @@ def test_one_row_of_any_stride():
     hch.hch_attn_fwd(c.code, t["q"], t["k"], t["v"], t["o"], c.lse, c.dqo, c.dko, None, hq, hkv, d, c.scale, c.ws)
     torch.cuda.synchronize()
     assert (np.abs(t["o"].double().cpu().numpy() - c.want["o"]) <= c.bounds()["o"]).all()
+
+
+def test_a_mask_that_is_no_tensor_is_refused():
+    c = Case("f32", [4], [6], 2, 1, 32)
+    with pytest.raises(hch.HchError) as e:
+        hch.hch_attn_fwd(c.code, c.t["q"], c.t["k"], c.t["v"], c.t["o"], c.lse, c.dqo, c.dko, np.ones(6, np.uint8), 2, 1, 32, 1.0, c.ws)
+    assert e.value.status == 1
