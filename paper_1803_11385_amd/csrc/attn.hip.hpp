@@ -677,13 +677,18 @@ __global__ __launch_bounds__((Keys<E, D, QW, VEC>::THREADS), (Keys<E, D, QW, VEC
                 for (int r = 0; r < 16; ++r) acc[dt][r] *= f;
         }
         const float base = m == -INFINITY ? 0.f : m;    // no key yet: exp2(-inf) = 0, not -inf + inf
+        // Weights are added up by tiles first: one by one, 300000 equal ones are rounded to the same side each time, 1e-3 of l in all
+        // (by tiles 1e-5; the sum with what each addition loses carried along 2e-6, but one register too many for fp32 of 96
+        // channels, 485 -> 578 us).
+        float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < S::NT; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[i][r] = exp2_fast(__builtin_fmaf(s[i][r], a.c, -base));
-                l += s[i][r];
+                sum += s[i][r];
             }
+        l += sum;
         __builtin_amdgcn_s_setprio(1);
         fold.run(s, acc);
         __builtin_amdgcn_s_setprio(0);

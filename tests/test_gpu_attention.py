@@ -392,3 +392,37 @@ def test_a_mask_that_is_no_tensor_is_refused():
     with pytest.raises(hch.HchError) as e:
         hch.hch_attn_fwd(c.code, c.t["q"], c.t["k"], c.t["v"], c.t["o"], c.lse, c.dqo, c.dko, np.ones(6, np.uint8), 2, 1, 32, 1.0, c.ws)
     assert e.value.status == 1
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 64])
+def test_sums_of_300000_nearly_equal_weights(dtype, d):
+    """Equal weights that are no power of two (the running maximum is that of the first keys, which score 3 less) are rounded to the
+    same side at every addition.  n weights are added in n / 32 steps after sums of 32, and n / 16 products' sums to o: the bound
+    takes their roundings as independent, 8 deviations wide, instead of adding n of them up.  Eight different queries, so many times
+    that the keys are not split."""
+    code, t = TYPES[dtype]
+    n, rows, heads, kinds = 300000, 65536, 2, 8
+    rng = np.random.default_rng(d)
+    on = lambda a: torch.from_numpy(a.astype(np.float32)).to(t)
+    e = rng.normal(size=d)
+    e /= np.linalg.norm(e)
+    k = 4.0 * np.repeat(e[None], n, 0)
+    k[:64] -= 3.0 * e
+    q, k, v = on(np.stack([e * (1 + 0.05 * i) for i in range(kinds)])), on(k + 1e-3 * rng.normal(size=k.shape)), on(rng.normal(size=(n, d)) + 0.5)
+    w = K.attention(q.float().numpy(), k.float().numpy(), v.float().numpy(), [0, kinds], [0, n], None, 1, 1, d, 1.0)
+    twice = lambda x: torch.cat([x, x], 1).cuda()
+    qs, ks, vs = twice(q.repeat(rows // kinds, 1)), twice(k), twice(v)
+    o, lse = torch.empty_like(qs), torch.empty((rows, heads), device="cuda")
+    off = [torch.tensor([0, x], dtype=torch.int32).cuda() for x in (rows, n)]
+    ws = _ws(hch.hch_attn_workspace_bytes(hch.HCH_WS_FWD, code, 1, rows, n, heads, heads, d))
+    names = _launched(lambda: hch.hch_attn_fwd(code, qs, ks, vs, o, lse, *off, None, heads, heads, d, 1.0, ws))
+    assert not any("join" in x for x in names), names
+    score = (d + 32) * U * w["top"] + 8 * U * (1 + np.log(n))
+    near = 8 * np.sqrt(n / 32) * U + 64 * U
+    got = lse.double().cpu().numpy().reshape(-1, kinds, heads)
+    assert np.abs(got - w["lse"][None]).max() <= score + near + 4 * U * np.abs(w["lse"]).max()
+    got = o.double().cpu().numpy().reshape(-1, kinds, heads, d)
+    b = EPS if dtype == "bf16" else 0.0
+    bound = (2 * score + near + 8 * np.sqrt(n / 16) * U + b) * w["o_abs"] + b * np.abs(w["o"])
+    assert (np.abs(got - w["o"][None, :, None]) <= bound[None, :, None]).all()
