@@ -49,7 +49,7 @@ struct Args {
     int batch, hq, hkv, group, d;
     int slots, splits, run, per_head;      // tiles per head at most, splits over the streamed rows; see work_item
     int vec;                               // everything in 16-byte pieces
-    int sorted;                            // units in the order of what streams past them, the longest first
+    int sorted;                            // units in the order of what streams past them, the longest first; of up to 64 shapes
     float scale, c;                        // c = scale log2(e)
 };
 
