@@ -307,15 +307,15 @@ class Levels:
             self._n[level] = int(self.info(level).n_total)
         return self._n[level]
 
-    def device_offsets(self, level):
-        """First row of each shape of `level`, and behind the last: [batch + 1] int32 on the GPU, as hch_attn_* take it."""
+    def device_offsets(self, level, device="cuda"):
+        """First row of each shape of `level`, and behind the last: [batch + 1] int32 on `device`, as hch_attn_* take it."""
         import torch
-        return torch.from_numpy(self.info(level).N.astype(np.int32)).cuda()
+        return torch.from_numpy(self.info(level).N.astype(np.int32)).to(device)
 
-    def device_positions(self, level):
-        """Voxel positions of `level` in data order, [n][3] int32 on the GPU, as hch_rope_* take them."""
+    def device_positions(self, level, device="cuda"):
+        """Voxel positions of `level` in data order, [n][3] int32 on `device`, as hch_rope_* take them."""
         import torch
-        return torch.from_numpy(self.info(level).coords_host()).cuda()
+        return torch.from_numpy(self.info(level).coords_host()).to(device)
 
     def free(self):
         if self._h:

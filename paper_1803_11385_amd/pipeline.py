@@ -158,7 +158,8 @@ class AttentionBlock:
         wq, wk, c = heads_q * head_dim, heads_kv * head_dim, channels
         f32 = dict(dtype=torch.float32, device=device)
         t = dict(dtype=torch.bfloat16 if dtype == B.HCH_BF16 else torch.float32, device=device)
-        self.offsets, self.positions, self.key_mask = levels.device_offsets(level), levels.device_positions(level), None
+        self.offsets, self.positions = levels.device_offsets(level, device), levels.device_positions(level, device)
+        self.key_mask = None
         self.field = torch.empty((n, 1), dtype=torch.int32, device=device)
         self.field_t = torch.empty((n, 1), dtype=torch.int32, device=device)
         B.hch_field_build(levels, level, 1, 1, 0, self.field, self.field_t)

@@ -148,3 +148,14 @@ def test_attention_refuses_launches_of_2_to_24_workgroups():
 def test_rope_refuses_launches_of_2_to_24_workgroups():
     f = hch.load_library().hch_rope_fwd
     assert f(0, P, 1 << 22, 0, 2 * P, 1 << 22, P, 1 << 28, 1 << 14, 1, 256, (C.c_int32 * 3)(1, 1, 1), 1e4, 1.0, None) == 5
+
+
+def test_offsets_and_positions_of_a_level_go_where_they_are_asked_for():
+    import numpy as np
+    import synth_shapes as S
+    coords, offs, _ = S.config_batch(2, batch=3, u=16)
+    lv = hch.hch_build_tables_host(coords, offs, 16, 2)
+    for level in range(2):
+        o, p = lv.device_offsets(level, "cpu"), lv.device_positions(level, "cpu")
+        assert o.device.type == p.device.type == "cpu"
+        assert o.dtype == p.dtype and o.tolist() == lv.info(level).N.tolist() and np.array_equal(p.numpy(), lv.info(level).coords_host())
