@@ -382,7 +382,8 @@ template <int D, int ROWS> struct Direct {
         }
     }
     // Written out, as the compiler would wait for all of them before the next transposing read of any part of LDS; that
-    // they have arrived is waited for in wait().  m0: where in LDS lane 0's piece goes.
+    // they have arrived is waited for in wait().  m0: where in LDS lane 0's piece goes; a reserved register, in which the compiler keeps
+    // nothing from one instruction to the next, and which a list of overwritten registers may not name.
     static __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t rs, int offset, char *to)
     {
         const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void *)(void *)to);
@@ -515,7 +516,7 @@ __device__ __forceinline__ void store_row(U *row, const f32x16 (&acc)[DT], float
         }
 }
 
-// Which of 64 keys from `key` on are there and seen.
+// Whether a key is there and seen: its byte of the mask, 1 without one.
 __device__ __forceinline__ int key_byte(const uint8_t *mask, int key, int end) { return key < end ? (mask ? (int)mask[key] : 1) : 0; }
 
 // Sizes of the passes over the keys.  QW wavefronts have rows of their own and KW share a row tile's keys: 4 x 1 (wide)

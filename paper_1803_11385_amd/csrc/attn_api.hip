@@ -58,7 +58,10 @@ Plans plan(const hch_attn_desc &p, int64_t rows, int rows_each, int heads, doubl
             double us = (START + std::ceil(UNEVEN * steps / splits) * st.us * cost) * busy;
             // Memory: at its rate if the compute units share evenly.  Shapes of different lengths do not split into equal parts, which
             // several workgroups a unit even out (one query for each of 8 shapes of 609323 keys together, 2 heads of 32, bf16: 256 workgroups 70 us,
-            // 512 42, 768 36, 1024 47; 304000 keys, 4 heads of 64: 93, 70, 65, 66).
+            // 512 42, 768 36, 1024 47; 304000 keys, 4 heads of 64: 93, 70, 65, 66).  Against a share of 1 this changes the choice for 243 of 1500
+            // drawn batches of 1 to 16 queries a shape; 100 of those take 0.96 of the time in the mean, uneven shapes 0.93 (0.65 to
+            // 1.18), equal ones, which are not known here, 1.06 (0.95 to 1.24).  A single shape beyond two rounds: 0.97 of the time in
+            // the middle of 40 (mostly 0.95 to 1.02).
             const double share = p.batch == 1 ? (each > 2.0 ? 1.1 : 1.0) : each <= 1.0 ? 1.45 : each <= 2.0 ? 1.12 : each <= 3.0 ? 1.0 : 1.1;
             const double move = moved / MEMORY * each * UNITS / (wgs * splits) * share;
             us = std::max(us, move) + 0.2 * std::min(us, move);         // (they do not overlap altogether)
