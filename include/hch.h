@@ -651,14 +651,15 @@ hch_status hch_qknorm_rope_bwd(hch_dtype x_dtype, const void *X, int64_t ld_x, h
  * step need two seeds.  What is dropped is 0 whatever it held (NaN and infinity included).
  * With the residual sum and the layer norm of hch_layernorm_fwd behind it, in one pass:
  *   s = r + k x;  Y = norm(s)       X, R, S  DEVICE [n][c] of x_dtype; S may be X or R;  the rest as there
+ *   Y may be X or R with one type, but not S
  * and back, from the rows S that were normalised and their stats:
- *   dR = gradient through the norm + dS (may be NULL)     DEVICE [n][c] of x_dtype; dR may be dS
+ *   dR = gradient through the norm + dS (may be NULL)     DEVICE [n][c] of x_dtype; may be S, dS, or dY with one type
  *   dX = k dR, before dR is rounded                       DEVICE [n][c] of dx_dtype; may be no other tensor of the call
  *   dgamma, dbeta, workspace as in hch_layernorm_bwd (hch_layernorm_workspace_bytes)
  * n = 0 is allowed, with null pointers for what has no rows.
  * Errors: HCH_EINVAL (null pointer, one of a pair alone, sizes negative, p outside [0, 1] or NaN, step not aligned to 8 bytes, in place
- * with another type, eps negative or NaN, unknown dtype, workspace misaligned), HCH_EUNSUPPORTED (more than 2^60 elements; with the norm,
- * c > 8192), HCH_EWORKSPACE, HCH_EHIP.
+ * with another type, dX or S in the place of another as above, eps negative or NaN, unknown dtype, workspace misaligned),
+ * HCH_EUNSUPPORTED (more than 2^60 elements; with the norm, c > 8192), HCH_EWORKSPACE, HCH_EHIP.
  */
 hch_status hch_dropout_fwd(hch_dtype x_dtype, const void *X, const void *R, hch_dtype y_dtype, void *Y, int64_t n, int32_t c,
                            float p, uint64_t seed, const int64_t *step, void *stream);

@@ -89,6 +89,8 @@ try {
     if (!known(x_dtype) || !known(y_dtype)) return fail(HCH_EINVAL, name + ": unknown dtype");
     if (n && (!X || !R || !S || !Y)) return fail(HCH_EINVAL, name + ": null pointer");
     if (n < 0 || c <= 0 || !(eps >= 0.f)) return fail(HCH_EINVAL, name + ": bad size or eps");
+    if (n && Y == S) return fail(HCH_EINVAL, name + ": S and Y are one tensor");
+    if (n && (Y == X || Y == R) && x_dtype != y_dtype) return fail(HCH_EINVAL, name + ": in place needs one type");
     hch::dropout::Drop drop;
     if (const hch_status st = drop_of(name, p, seed, step, drop)) return st;
     if (c > MAX_CHANNELS) return fail(HCH_EUNSUPPORTED, name + ": more than 8192 channels");
@@ -123,7 +125,8 @@ try {
     if ((n && (!S || !stats || !dY || !dR || !dX)) || (dgamma != nullptr) != (dbeta != nullptr))
         return fail(HCH_EINVAL, name + ": null pointer, or only one of dgamma and dbeta");
     if (n < 0 || c <= 0) return fail(HCH_EINVAL, name + ": bad size");
-    if (n && dR == dX) return fail(HCH_EINVAL, name + ": dR and dX are one tensor");
+    if (n && (dX == dR || dX == S || dX == dY || dX == dS)) return fail(HCH_EINVAL, name + ": dX is another tensor of the call too");
+    if (n && dR == dY && x_dtype != dy_dtype) return fail(HCH_EINVAL, name + ": in place needs one type");
     hch::dropout::Drop drop;
     if (const hch_status st = drop_of(name, p, seed, step, drop)) return st;
     if (c > MAX_CHANNELS) return fail(HCH_EUNSUPPORTED, name + ": more than 8192 channels");

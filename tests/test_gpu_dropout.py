@@ -185,6 +185,42 @@ def test_dropout_with_sum_and_norm(x, y, dx, c):
                 assert torch.equal(s2, S) and torch.equal(y2, Y)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [50, 64, 63, 1030, 4097])
+def test_results_in_the_place_of_arguments(dtype, c):
+    """The same bits as in tensors of their own: each lane has read what it overwrites."""
+    rng = np.random.default_rng(c)
+    code, n, p, seed = TYPES[dtype][0], 3001 if c < 100 else 301, 0.3, 2 ** 64 - 9
+    (X, _), (Rr, _), (DY, _), (DS, _) = (_on(rng, (n, c), dtype) for _ in range(4))
+    at, stats = _step(7), torch.empty((n, 2), device="cuda")
+    new = lambda: torch.full((n, c), float("nan"), dtype=TYPES[dtype][1], device="cuda")
+
+    want = new()
+    hch.hch_dropout_bwd(code, DY, code, want, n, c, p, seed, at)
+    Z = DY.clone()
+    hch.hch_dropout_bwd(code, Z, code, Z, n, c, p, seed, at)                # dx = dy
+    assert torch.equal(Z, want)
+
+    S, Y = new(), new()
+    hch.hch_dropout_layernorm_fwd(code, X, Rr, S, None, None, code, Y, stats, n, c, 1e-5, p, seed, at)
+    for k in range(2):                                                      # y = x, y = r; and s in the other's place
+        for s_there in (False, True):
+            a, r = X.clone(), Rr.clone()
+            y, s = (a, r) if k == 0 else (r, a)
+            s = s if s_there else new()
+            hch.hch_dropout_layernorm_fwd(code, a, r, s, None, None, code, y, None, n, c, 1e-5, p, seed, at)
+            assert torch.equal(y, Y) and torch.equal(s, S)
+
+    dR, dX, dg, db = new(), new(), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    ws = torch.full((hch.hch_layernorm_workspace_bytes(n, c),), 255, dtype=torch.uint8, device="cuda")
+    hch.hch_dropout_layernorm_bwd(code, S, stats, None, code, DY, DS, dR, code, dX, dg, db, n, c, p, seed, at, ws)
+    for k in range(3):                                                      # dr = s, dy, ds
+        s, dy, ds = S.clone(), DY.clone(), DS.clone()
+        r2, x2, dg2, db2 = (s, dy, ds)[k], new(), torch.empty_like(dg), torch.empty_like(db)
+        hch.hch_dropout_layernorm_bwd(code, s, stats, None, code, dy, ds, r2, code, x2, dg2, db2, n, c, p, seed, at, ws)
+        assert torch.equal(r2, dR) and torch.equal(x2, dX) and torch.equal(dg2, dg) and torch.equal(db2, db)
+
+
 def test_one_mask_in_all_calls():
     """Alone and with the norm, in every type and at every alignment."""
     for c in (24, 50, 63, 1026):

@@ -87,6 +87,25 @@ def test_dropout_refuses():
     assert _norm_bwd(n=0, X=None, st=None, Y=None, dR=None, dX=None, dg=None, db=None, ws=None, nb=0) == 0
 
 
+def test_dropout_with_norm_refuses_tensors_that_overwrite_each_other():
+    """Rows of one type in place of rows of another are written over rows that other workgroups have still to read; Y in S's place, and dX in
+    that of any other tensor, leave one result where two are promised."""
+    def bwd(t=0, S=P, u=0, dY=2 * P, dS=None, dR=3 * P, v=0, dX=4 * P, n=4):
+        return hch.load_library().hch_dropout_layernorm_bwd(t, S, P, None, u, dY, dS, dR, v, dX, None, None, n, 8, 0.1, 0, None, None, 0, None)
+
+    for t, u in ((0, 1), (1, 0)):
+        assert _norm_fwd(t=t, u=u, Y=P) == 1 and _norm_fwd(t=t, u=u, Y=2 * P) == 1 and _norm_fwd(t=t, u=u, Y=3 * P) == 1
+        assert bwd(t=t, u=u, dR=2 * P) == 1
+    for t in (0, 1):
+        assert _norm_fwd(t=t, u=t, Y=3 * P) == 1 and _norm_fwd(t=t, u=t, S=P, Y=P) == 1 and _norm_fwd(t=t, u=t, S=2 * P, Y=2 * P) == 1
+        for v in (0, 1):
+            assert bwd(t=t, v=v, dX=P) == 1 and bwd(t=t, u=v, v=v, dX=2 * P) == 1 and bwd(t=t, v=v, dS=5 * P, dX=5 * P) == 1
+            assert bwd(t=t, v=v, dX=3 * P) == 1
+    assert b"hch_dropout_layernorm_bwd" in hch.load_library().hch_last_error()
+    assert bwd(n=0, S=None, dY=None, dR=None, dX=None) == 0 and bwd(n=0, S=P, dY=P, dR=P, dX=P) == 0
+    assert _norm_fwd(n=0, X=P, R=P, S=P, Y=P, u=1) == 0
+
+
 def _embed(t=0, T=P, ids=P, u=0, Y=P, ld=8, n=4, c=8, vocab=10, scale=1.0):
     return hch.load_library().hch_embed_fwd(t, T, ids, u, Y, ld, n, c, vocab, scale, None)
 
