@@ -5,7 +5,8 @@
 // Gradient: no atomics on the table, whose order would change the bits from run to run.  Rows are sorted by label (stable, by
 // digits of 6 to 9 bits, as many as the table's size needs), a group of lanes adds up to 16 rows of that order, a workgroup joins its
 // groups' runs, and a last launch those that go over several workgroups.  So the work is spread by rows, whatever labels
-// they have, and a label that most rows have costs no more than others.  Sums are fp32, of 16 rows and then by trees.
+// they have, and a label that most rows have costs no more than others.  Sums are fp32: of 16 rows, by trees over a
+// workgroup's rows, and over workgroups in blocks of 64.
 // 609323 rows of 64, bf16, 32768 labels: 56 us: two passes of the sort 33, the rows 24 (18 at a copy's rate: they are read 128 bytes here and
 // there, and the table is cleared first), the join 5.  63331 rows of 50, fp32, 50 labels: 17 us, four launches of 3 to 7 us that wait for memory, not for its
 // rate (2.6).  Tried and not kept: sums of a small table's labels in LDS, a thread's own by LDS additions, which take 200 cycles a row (609323
@@ -481,10 +482,14 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(Runs R, const TY *dY
 }
 
 // Runs that go over several tiles: the tile in which one ends adds up its parts, in the tiles' order by as many chains as a workgroup has room
-// for and a tree over them.  `lanes` threads have a row's pieces of N channels.
+// for and a tree over them.  `lanes` threads have a row's pieces of N channels.  A chain's parts are added up by BLOCK, and those sums behind each other:
+// what additions round away has one sign where rows are alike, and grows with their number (200001 like rows of 1031, fp32, one label, 3126 parts in a
+// chain: off by up to 4.6e-5 part by part, 1.6e-6 so; as fast where AHEAD parts are read before they are added, 40000 rows of 1030, bf16, one label 182 us, 180
+// part by part).
 template <int N> __global__ __launch_bounds__(JOIN) void embed_join_kernel(Runs R, float *dT, int c, int rows, float scale, int lanes)
 {
     typedef float V __attribute__((ext_vector_type(N)));
+    constexpr int BLOCK = 64, AHEAD = 8;
     __shared__ V lds[JOIN];
     const int64_t tile = blockIdx.x;
     const int32_t label = R.pairs[tile * rows].x, ends = R.ends[tile];        // read at once; they say nothing behind the last row
@@ -494,9 +499,25 @@ template <int N> __global__ __launch_bounds__(JOIN) void embed_join_kernel(Runs 
     for (int piece1 = 0; piece1 < pieces; piece1 += lanes) {
         const int piece = piece1 + piece0;
         V t = {};
-        if (piece < pieces)
+        if (piece < pieces) {
+            auto part = [&](int64_t i) { return *(const V *)(R.part + ((first + i) * 2 + (i == 0)) * c + piece * N); };
+            int64_t i = group;
+            while (i + (int64_t)(BLOCK - 1) * groups < count) {
+                V b = {};
+                for (int k = 0; k < BLOCK; k += AHEAD, i += AHEAD * groups) {
+                    V v[AHEAD];
+#pragma unroll
+                    for (int j = 0; j < AHEAD; ++j) v[j] = part(i + j * groups);
+#pragma unroll
+                    for (int j = 0; j < AHEAD; ++j) b += v[j];
+                }
+                t += b;
+            }
+            V b = {};
 #pragma unroll 8
-            for (int64_t i = group; i < count; i += groups) t += *(const V *)(R.part + ((first + i) * 2 + (i == 0)) * c + piece * N);
+            for (; i < count; i += groups) b += part(i);
+            t += b;
+        }
         lds[threadIdx.x] = t;
         __syncthreads();
         int half = groups / 2;

@@ -120,6 +120,25 @@ def test_more_tiles_than_a_workgroup_counts(kind, vocab):
     _gradient(rng, _ids(rng, 8192 * 160 + 4321, vocab, kind), vocab, 3, "f32")
 
 
+@pytest.mark.parametrize("y,n,c,rows,chains", [("bf16", 609323, 1030, 64, 1), ("f32", 200001, 1031, 64, 1), ("f32", 152343, 256, 64, 4), ("bf16", 2 ** 22, 64, 512, 16)])
+def test_long_runs_of_like_rows(y, n, c, rows, chains):
+    """All rows alike, with one label: what each addition rounds away has the same sign, so that errors add up.  A value passes 16 additions in a group's
+    rows, 6 at most from group to group and 4 from wavefront to wavefront, 64 in a block of the join's chain, as many as that chain has blocks, and
+    those that join the chains; then the scale."""
+    vocab = 2
+    row = torch.from_numpy((0.5 + np.random.default_rng(c).random(c)).astype(np.float32)).to(TYPES[y][1]).cuda()
+    dY = row.expand(n, c).contiguous()
+    ids = torch.ones(n, dtype=torch.int32, device="cuda")
+    dT = torch.full((vocab, c), float("nan"), device="cuda")
+    hch.hch_embed_bwd(ids, TYPES[y][0], dY, dT, n, c, vocab, 0.3, _ws(n, c, vocab))
+    want = n * float(np.float32(0.3)) * row.double().cpu().numpy()
+    parts = -(-n // rows)
+    depth = 16 + 6 + 4 + 64 + -(-parts // (64 * chains)) + chains.bit_length() + 1
+    _near(dT, np.stack([0 * want, want]), depth * U * np.stack([want, want]), "dtable")
+    del dY
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("c,tile", [(4, 1024), (40, 256), (64, 256), (200, 64)])
 def test_runs_at_the_borders_of_groups_wavefronts_and_tiles(c, tile):
     """Runs that begin and end before, on and behind the borders of 16 rows, of a wavefront's rows and of a workgroup's, in every
