@@ -221,6 +221,28 @@ def test_results_in_the_place_of_arguments(dtype, c):
         assert torch.equal(r2, dR) and torch.equal(x2, dX) and torch.equal(dg2, dg) and torch.equal(db2, db)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c", [(100003, 50), (100003, 64), (200001, 3), (20011, 250), (3001, 1030), (2003, 4097)])
+def test_sums_over_many_rows_are_exact_where_they_are_whole(dtype, n, c):
+    """Rows of +-1 that are normalised already (mean 0, deviation 1) and dy of 1 .. 7 with their sign, or all positive: every term of a
+    sum is a positive whole number and sums stay below 2^24, so that they are exact in any order, and a row lost, taken twice or taken for
+    another's shows."""
+    rng = np.random.default_rng(n + c)
+    sign = torch.from_numpy(rng.choice([-1.0, 1.0], (n, c)).astype(np.float32))
+    size = torch.from_numpy(rng.integers(1, 8, (n, c)).astype(np.float32))
+    S = sign.to(TYPES[dtype][1]).cuda()
+    stats = torch.tensor([0.0, 1.0], device="cuda").repeat(n, 1)
+    dR, dX = torch.empty_like(S), torch.empty_like(S)
+    dg, db = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    ws = torch.full((hch.hch_layernorm_workspace_bytes(n, c),), 255, dtype=torch.uint8, device="cuda")
+    want = size.double().sum(0)
+    for signed in (True, False):
+        dY = (size * sign if signed else size).to(TYPES[dtype][1]).cuda()
+        hch.hch_dropout_layernorm_bwd(TYPES[dtype][0], S, stats, None, TYPES[dtype][0], dY, None, dR, TYPES[dtype][0], dX, dg, db, n, c, 0.1, 3, None, ws)
+        assert torch.equal((dg if signed else db).double().cpu(), want)
+        assert torch.equal((db if signed else dg).double().cpu(), (size * sign).double().sum(0))
+
+
 def test_one_mask_in_all_calls():
     """Alone and with the norm, in every type and at every alignment."""
     for c in (24, 50, 63, 1026):

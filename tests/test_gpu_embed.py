@@ -120,6 +120,49 @@ def test_more_tiles_than_a_workgroup_counts(kind, vocab):
     _gradient(rng, _ids(rng, 8192 * 160 + 4321, vocab, kind), vocab, 3, "f32")
 
 
+def _exact_gradient(rng, ids, vocab, c, y, scale=0.5):
+    """Rows of 1 .. 7, positive, and a scale of a power of two: sums are whole numbers below 2^24 times the scale, exact in any order; a row lost, taken
+    twice or under another's label shows, however long its run."""
+    n = ids.size
+    made = torch.Generator(device="cuda").manual_seed(int(rng.integers(2 ** 31)))
+    rows = torch.randint(1, 8, (n, c), generator=made, device="cuda").float()
+    assert 7 * n < 2 ** 24
+    I = torch.from_numpy(ids).cuda()
+    sums = torch.zeros((n + 1, c), dtype=torch.float64, device="cuda")
+    by_label, order = torch.sort(I.long())
+    torch.cumsum(rows[order].double(), 0, out=sums[1:])    # whole numbers: exact
+    ends = torch.searchsorted(by_label, torch.arange(-1, vocab, device="cuda"), right=True)
+    want = sums[ends[1:]] - sums[ends[:-1]]
+    dT = torch.full((vocab, c), float("nan"), device="cuda")
+    hch.hch_embed_bwd(I, TYPES[y][0], rows.to(TYPES[y][1]), dT, n, c, vocab, scale, _ws(n, c, vocab))
+    wrong = (dT.double() != scale * want).any(1)
+    assert not wrong.any(), f"{n} rows of {c}: {int(wrong.sum())} of {vocab} labels, the first {int(wrong.nonzero()[0])}"
+
+
+@pytest.mark.parametrize("kind,vocab", [("one", 1), ("one", 700), ("skewed", 2), ("skewed", 65), ("gaps", 2), ("skewed", 40000), ("blocks", 10 ** 5)])
+@pytest.mark.parametrize("y,c", [("f32", 20), ("bf16", 64), ("f32", 7), ("bf16", 16), ("f32", 1), ("f32", 200), ("f32", 257), ("bf16", 256)])
+def test_long_runs_are_exact_where_sums_are_whole(kind, vocab, y, c):
+    rng = np.random.default_rng(c)
+    for n in (64 * 33 + 1, 200001):
+        _exact_gradient(rng, _ids(rng, n, vocab, kind), vocab, c, y)
+
+
+@pytest.mark.parametrize("kind,vocab", [("gaps", 3000), ("one", 40), ("skewed", 2), ("skewed", 300000)])
+@pytest.mark.parametrize("y,c", [("f32", 3), ("bf16", 64)])
+def test_many_tiles_are_exact_where_sums_are_whole(kind, vocab, y, c):
+    """On both sides of the lines at which a thread of the sort has more rows and the tiles' counts are added up by a launch of their own."""
+    rng = np.random.default_rng(c)
+    for n in (163840, 163841, 327681, 655360, 655361, 8192 * 160 + 4321):
+        _exact_gradient(rng, _ids(rng, n, vocab, kind), vocab, c, y)
+
+
+@pytest.mark.parametrize("y,c", [("f32", 1030), ("bf16", 1030), ("f32", 1031), ("bf16", 2048)])
+@pytest.mark.parametrize("kind,vocab", [("one", 3), ("skewed", 5)])
+def test_long_runs_of_wide_rows_are_exact_where_sums_are_whole(kind, vocab, y, c):
+    rng = np.random.default_rng(c)
+    _exact_gradient(rng, _ids(rng, 40009, vocab, kind), vocab, c, y)
+
+
 @pytest.mark.parametrize("y,n,c,rows,chains", [("bf16", 609323, 1030, 64, 1), ("f32", 200001, 1031, 64, 1), ("f32", 152343, 256, 64, 4), ("bf16", 2 ** 22, 64, 512, 16)])
 def test_long_runs_of_like_rows(y, n, c, rows, chains):
     """All rows alike, with one label: what each addition rounds away has the same sign, so that errors add up.  A value passes 16 additions in a group's

@@ -155,6 +155,25 @@ def test_longer_than_one_wave_of_workgroups():
     _check(np.random.default_rng(2), 30011, 4, 2, 1, 20, (4, 3, 3), "f32", "bf16", "f32")
 
 
+@pytest.mark.parametrize("x,y", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16")])
+@pytest.mark.parametrize("n,heads,hq,hk,d", [(30011, 3, 1, 1, 64), (30011, 6, 4, 2, 16), (200003, 2, 1, 1, 32), (50021, 3, 2, 0, 128), (20021, 4, 2, 1, 256)])
+def test_sums_over_many_rows_are_exact_where_they_are_whole(x, y, n, heads, hq, hk, d):
+    """Heads of +-1 without positions, eps 0: u = x.  dy is 1 .. 7 with the sign of x, so that every term of gamma's gradient is a positive whole
+    number and sums stay below 2^24: exact in any order, and a head or row lost, taken twice or taken for another's shows."""
+    rng = np.random.default_rng(n + d)
+    sign = torch.from_numpy(rng.choice([-1.0, 1.0], (n, heads, d)).astype(np.float32))
+    size = torch.from_numpy(rng.integers(1, 8, (n, heads, d)).astype(np.float32))
+    X = sign.to(TYPES[x][1]).cuda().view(n, -1)
+    dY = (size * sign).to(TYPES[y][1]).cuda().view(n, -1)
+    dX = torch.empty_like(X)
+    dgq, dgk = (torch.full((d,), float("nan"), device="cuda") for _ in range(2))
+    co = torch.zeros((n, 3), dtype=torch.int32, device="cuda")
+    ws = torch.full((hch.hch_qknorm_rope_workspace_bytes(n, hq, hk, d),), 255, dtype=torch.uint8, device="cuda")
+    hch.hch_qknorm_rope_bwd(TYPES[x][0], X, TYPES[y][0], dY, TYPES[x][0], dX, None, None, dgq, dgk, co, n, heads, hq, hk, d, (0, 0, 0), ws, eps=0.0)
+    assert torch.equal(dgq.double().cpu(), size[:, :hq].double().sum((0, 1)))
+    assert torch.equal(dgk.double().cpu(), size[:, hq: hq + hk].double().sum((0, 1)))
+
+
 def test_heads_of_zeros_and_tiny_ones():
     n, d = 6, 64
     X = torch.zeros((n, 3 * d), device="cuda")
