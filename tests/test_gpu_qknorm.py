@@ -155,6 +155,60 @@ def test_longer_than_one_wave_of_workgroups():
     _check(np.random.default_rng(2), 30011, 4, 2, 1, 20, (4, 3, 3), "f32", "bf16", "f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,heads,hq,hk,d", [(1, 3, 1, 1, 64), (45, 5, 2, 2, 40), (3001, 6, 3, 1, 32), (2000, 3, 2, 1, 66), (5000, 4, 0, 2, 16)])
+@pytest.mark.parametrize("ld_more,offset", [(0, 0), (16, 0), (4, 4), (2, 2), (3, 1)])
+def test_results_in_the_place_of_arguments(dtype, n, heads, hq, hk, d, ld_more, offset):
+    """The same bits as in tensors of their own, also in columns of wider rows, whose other columns stay."""
+    rng = np.random.default_rng(n)
+    w, ld, code = heads * d, heads * d + ld_more, TYPES[dtype][0]
+    sections = (d // 2 - 2 * (d // 6), d // 6, d // 6)
+    gq, gk = torch.randn(d, device="cuda"), torch.randn(d, device="cuda")
+    co = torch.from_numpy(rng.integers(0, 64, (n, 3)).astype(np.int32)).cuda()
+    ws = torch.full((hch.hch_qknorm_rope_workspace_bytes(n, hq, hk, d),), 255, dtype=torch.uint8, device="cuda")
+    place = (co, n, heads, hq, hk, d, sections)
+
+    def rows():
+        t, _, whole = _rows(rng, n, w, ld, offset, dtype)
+        return t, whole
+
+    def twin(whole):
+        whole = whole.clone()
+        return whole[offset:].view(n, ld)[:, :w], whole
+
+    def rest_stays(whole):
+        between = whole.clone()
+        between[offset:].view(n, ld)[:, :w] = -7.0
+        assert (between == -7).all()
+
+    (X, xw), (dY, yw), (Y, _) = rows(), rows(), rows()
+    hch.hch_qknorm_rope_fwd(code, X, code, Y, gq, gk, *place)
+    Z, zw = twin(xw)
+    hch.hch_qknorm_rope_fwd(code, Z, code, Z, gq, gk, *place)
+    assert torch.equal(Z, Y)
+    rest_stays(zw)
+
+    dX, _ = rows()
+    dg = [torch.full((d,), float("nan"), device="cuda") for _ in range(2)]
+    hch.hch_qknorm_rope_bwd(code, X, code, dY, code, dX, gq, gk, *dg, *place, ws)
+    assert dX.isfinite().all()
+    for over in ("dY", "X"):
+        (x, x_), (dy, y_) = twin(xw), twin(yw)
+        out, whole = (dy, y_) if over == "dY" else (x, x_)
+        got = [torch.full((d,), float("nan"), device="cuda") for _ in range(2)]
+        hch.hch_qknorm_rope_bwd(code, x, code, dy, code, out, gq, gk, *got, *place, ws)
+        assert torch.equal(out, dX), over
+        rest_stays(whole)
+        # in dY's place values' heads are not walked through, so that rows may be in other workgroups: both orders have no more than 64 terms in a lane,
+        # 64 groups of lanes and 40 sums of workgroups behind each other
+        u = X.double().cpu().numpy().reshape(n, heads, d)
+        u = np.abs(u) / np.sqrt((u ** 2).mean(2, keepdims=True) + EPS)
+        terms = u * _lengths(dY.double().cpu().numpy(), d).reshape(n, heads, d)
+        for a, b, first, count in zip(got, dg, (0, hq), (hq, hk)):
+            assert torch.equal(a, b) if over == "X" else True
+            _near(a, b.double().cpu().numpy(), 2 * 168 * U * terms[:, first: first + count].sum((0, 1)), "dgamma")
+
+
 @pytest.mark.parametrize("x,y", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16")])
 @pytest.mark.parametrize("n,heads,hq,hk,d", [(30011, 3, 1, 1, 64), (30011, 6, 4, 2, 16), (200003, 2, 1, 1, 32), (50021, 3, 2, 0, 128), (20021, 4, 2, 1, 256)])
 def test_sums_over_many_rows_are_exact_where_they_are_whole(x, y, n, heads, hq, hk, d):
