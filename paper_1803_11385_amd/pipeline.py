@@ -271,10 +271,14 @@ class Embedding:
 
     @staticmethod
     def _type(t):
-        return B.HCH_F32 if t.dtype == torch.float32 else B.HCH_BF16
+        if t.dtype == torch.float32:
+            return B.HCH_F32
+        if t.dtype == torch.bfloat16:
+            return B.HCH_BF16
+        raise B.HchError(1, f"rows of an embedding: wrong element type {t.dtype}, fp32 or bf16 is needed")
 
     def forward(self, Y):
-        """Y [n][channels], or columns of wider rows (beside the features of an encoder's input, say)"""
+        """Y [n][channels] of fp32 or bf16, or columns of wider rows (beside the features of an encoder's input, say)"""
         B.hch_embed_fwd(self.dtype, self.table, self.ids, self._type(Y), Y, self.n, self.c, self.vocab, self.scale)
 
     def backward(self, dY):

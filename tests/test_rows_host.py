@@ -165,3 +165,17 @@ def test_tensors_of_another_gpu_are_refused(monkeypatch):
     assert binding._on(77, There(1), None, There(1)) == 77
     with pytest.raises(hch.HchError, match="GPU 0"):
         binding._on(77, There(1), There(0))
+
+
+def test_embedding_refuses_rows_of_other_types():
+    """Rows of fp16 or of integers are as wide as rows of bf16: their bits would be taken for bf16's."""
+    import torch
+    from paper_1803_11385_amd import pipeline
+    emb = pipeline.Embedding(4, 9, 8, device="cpu")
+    for call in (emb.forward, emb.backward):
+        for t in (torch.float16, torch.int16, torch.uint8, torch.float64):
+            with pytest.raises(hch.HchError, match=f"element type {t}"):
+                call(torch.zeros((4, 8), dtype=t))
+        for t in (torch.float32, torch.bfloat16):               # goes on to where the tensor's place is looked at
+            with pytest.raises(hch.HchError, match="GPU memory"):
+                call(torch.zeros((4, 8), dtype=t))
