@@ -147,12 +147,15 @@ class AttentionBlock:
     allocated once here; key_mask (bytes, nonzero = seen) may be set between passes.
 
     qk_norm: each head of q and k is divided by its root mean square and multiplied by gamma_q or gamma_k before it is turned.
-    dropout (None: not built in): what the attention adds to X is dropped with this probability; the numbers come from `seed`, another for
-    each block, and `step` on the device, to which the program adds one for each training step (in a captured graph too).  A
-    forward pass and its backward pass take the same step.  `dropout` may be set between passes, 0 for evaluation."""
+    dropout (None: not built in): what the attention adds to X is dropped with this probability; the numbers come from `seed`, without a
+    default because blocks with one seed drop the same elements, and from `step` on the device, to which the program adds one for each
+    training step (in a captured graph too).  A forward pass and its backward pass take the same step.  `dropout` may be set
+    between passes, 0 for evaluation."""
 
     def __init__(self, levels, level, channels, heads_q, heads_kv, head_dim, dtype=B.HCH_F32, sections=None, base=10000.0,
-                 eps=1e-5, device="cuda", qk_norm=False, dropout=None, seed=0):
+                 eps=1e-5, device="cuda", qk_norm=False, dropout=None, seed=None):
+        if dropout is not None and (seed is None or not 0 <= seed < 2 ** 64):
+            raise B.HchError(1, "a block with dropout needs a seed of its own, 64 bits without a sign")
         self.levels, self.level, self.c, self.dtype = levels, level, channels, dtype
         self.hq, self.hkv, self.d, self.eps, self.base = heads_q, heads_kv, head_dim, eps, base
         third = head_dim // 6

@@ -179,3 +179,27 @@ def test_embedding_refuses_rows_of_other_types():
         for t in (torch.float32, torch.bfloat16):               # goes on to where the tensor's place is looked at
             with pytest.raises(hch.HchError, match="GPU memory"):
                 call(torch.zeros((4, 8), dtype=t))
+
+
+def test_a_block_with_dropout_needs_a_seed():
+    """Blocks with one seed drop the same elements in every step: none is taken that the program did not choose."""
+    from paper_1803_11385_amd import pipeline
+
+    class Reached(Exception):
+        pass
+
+    class Levels:
+        def n(self, level):
+            raise Reached
+
+    for p in (0.1, 0.0):
+        with pytest.raises(hch.HchError, match="seed"):
+            pipeline.AttentionBlock(Levels(), 0, 32, 2, 2, 16, dropout=p)
+        for seed in (-1, 2 ** 64):
+            with pytest.raises(hch.HchError, match="seed"):
+                pipeline.AttentionBlock(Levels(), 0, 32, 2, 2, 16, dropout=p, seed=seed)
+        for seed in (0, 2 ** 64 - 1):
+            with pytest.raises(Reached):
+                pipeline.AttentionBlock(Levels(), 0, 32, 2, 2, 16, dropout=p, seed=seed)
+    with pytest.raises(Reached):
+        pipeline.AttentionBlock(Levels(), 0, 32, 2, 2, 16)
