@@ -8,8 +8,10 @@ namespace {
 constexpr int64_t MAX_ROWS = (int64_t(1) << 31) - 4096;
 
 // Rows of a tile of the sort for each of its threads: few, so that many workgroups share the work, and so many that a workgroup can add up all
-// tiles' counts (up to TILES) by itself; beyond, where a thread has 8, a launch of its own does (609323 rows, 32768 labels: 75 tiles 71 us, 149 57, 298,
-// counted by a launch, 67).  8192 rows are one tile, sorted in one launch.
+// tiles' counts (up to TILES) by itself; beyond, where a thread has 8, a launch of its own does (609323 rows of 64, bf16, 32768 labels: 75 tiles 69 us, 149 56, 298,
+// counted by a launch, 66).  What the lines cost, the last call before each and the first behind it: 163840 rows 33.8 and 35.5 us, 327680 40.7 and 45.4,
+// 655360 58.0 and 70.2 (with 4 rows a thread, and a launch that counts 161 tiles, 58.1; 900000 rows 82.5, so 72.7).  8192 rows are one tile,
+// sorted in one launch (32.1 us; 8193 rows by several 26.1).
 constexpr int TILES = 160;
 int items_of(int64_t n)
 {
@@ -73,8 +75,8 @@ try {
     const int st = size_of(table_dtype), sy = size_of(y_dtype);
     int run = st + sy < 8 ? 8 : 4;         // 16 bytes of the shorter type
     while (run > 1 && (c % run || ld_y % run || !aligned(table, std::min(16, run * st)) || !aligned(Y, std::min(16, run * sy)))) run /= 2;
-    // where a thread would write less than 8 bytes, rows that lie one behind the other are written 16 bytes at a time (609323 rows, to bf16, of 50: 24 -> 19
-    // us, of 63: 48 -> 37)
+    // where a thread would write less than 8 bytes, rows that lie one behind the other are written 16 bytes at a time (609323 rows, from 4096 labels of fp32 to
+    // bf16, of 50: 24 -> 19 us, of 63: 48 -> 43, from bf16 48 -> 37)
     const bool flat = run * sy < 8 && c >= 8 && ld_y == c && aligned(Y, 16);
     const int64_t units = n * (c / run), each = hch::embed::THREADS * hch::embed::AT_ONCE;
     const unsigned grid = (unsigned)std::min<int64_t>((units - 1) / each + 1, 1 << 16);

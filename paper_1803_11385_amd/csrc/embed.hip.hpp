@@ -4,9 +4,10 @@
 // rows of 64 from 4096 labels, fp32 to bf16: 16 us, 5.1 TB/s.
 // Gradient: no atomics on the table, whose order would change the bits from run to run.  Rows are sorted by label (stable, by
 // digits of 6 to 9 bits, as many as the table's size needs), a group of lanes adds up to 16 rows of that order, a workgroup joins its
-// groups' runs, and a last launch those that go over several workgroups.  So the work is spread by rows, whatever labels
-// they have, and a label that most rows have costs no more than others.  Sums are fp32: of 16 rows, by trees over a
-// workgroup's rows, and over workgroups in blocks of 64.
+// groups' runs, and a last launch those that go over several workgroups.  So up to there the work is spread by rows, whatever
+// labels they have; but the parts of one label's run are added up by one workgroup, which tells where a run has hundreds of them: 609323 rows of 64, bf16,
+// of one label 38 us, of 4096 labels 50; 152343 of 256, fp32, 81 and 57; 40000 of 1030, bf16, 147 and 56.  Sums are fp32: of 16 rows, by trees over a
+// workgroup's rows, and over workgroups by chains in blocks of 64 and a tree over the chains.
 // 609323 rows of 64, bf16, 32768 labels: 56 us: two passes of the sort 33, the rows 24 (18 at a copy's rate: they are read 128 bytes here and
 // there, and the table is cleared first), the join 5.  63331 rows of 50, fp32, 50 labels: 17 us, four launches of 3 to 7 us that wait for memory, not for its
 // rate (2.6).  Tried and not kept: sums of a small table's labels in LDS, a thread's own by LDS additions, which take 200 cycles a row (609323
@@ -343,8 +344,8 @@ template <typename T, int W, int RUN> struct Raw {        // a lane's channels a
     type v[W / RUN];
 };
 
-// rows that a group of LPR lanes adds up: 16, fewer where groups are many, so that a workgroup has 1024 at most (98963 rows of 4 channels: a lane a row, four rows
-// each, 6.6 us; four lanes, of which three have nothing, 16 rows each, 12.5)
+// rows that a group of LPR lanes adds up: 16, fewer where groups are many, so that a workgroup has 1024 at most (98963 rows of 4 channels, 4178 labels, the whole
+// gradient: a lane a row, four rows each, 24.4 us; four lanes, of which three have nothing, 16 rows each, 26.5)
 constexpr int sub(int lpr) { return lpr >= 4 ? 16 : 4 * lpr; }
 
 // A workgroup has a tile of GROUPS * SUB rows of the sorted order, LPR * W channels of them (blockIdx.y); a group of LPR lanes adds up SUB rows, all
@@ -484,8 +485,8 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(Runs R, const TY *dY
 // Runs that go over several tiles: the tile in which one ends adds up its parts, in the tiles' order by as many chains as a workgroup has room
 // for and a tree over them.  `lanes` threads have a row's pieces of N channels.  A chain's parts are added up by BLOCK, and those sums behind each other:
 // what additions round away has one sign where rows are alike, and grows with their number (200001 like rows of 1031, fp32, one label, 3126 parts in a
-// chain: off by up to 4.6e-5 part by part, 1.6e-6 so; as fast where AHEAD parts are read before they are added, 40000 rows of 1030, bf16, one label 182 us, 180
-// part by part).
+// chain: off by up to 4.6e-5 part by part, 1.6e-6 so).  AHEAD parts are on their way at once (one label, 40000 rows of 1030, bf16: 148 us, part by part 149;
+// 152343 of 256, fp32: 81 and 79).
 template <int N> __global__ __launch_bounds__(JOIN) void embed_join_kernel(Runs R, float *dT, int c, int rows, float scale, int lanes)
 {
     typedef float V __attribute__((ext_vector_type(N)));

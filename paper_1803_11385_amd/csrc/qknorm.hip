@@ -5,8 +5,8 @@
 
 namespace {
 
-// Workgroups of the backward pass at most, each with sums of its own: five on a compute unit, as many as registers allow (9533 rows of 24 heads of 64, bf16:
-// four 26 us, five 23.5; 46514 of 16 of 128: five 108, six, of which the last wait for the first, 133).
+// Workgroups of the backward pass at most, each with sums of its own: five on a compute unit, as many as registers allow (46514 rows of 16 heads of 128, bf16:
+// four 105 us, five 107, six, of which the last wait for the first, 128; 9533 of 24 of 64: 23.8, 24.3 and 26.8).
 constexpr int PARTS = 1280;
 
 struct HeadTensor { const void *p; int64_t ld; int bytes; };
@@ -18,8 +18,9 @@ bool whole(std::initializer_list<HeadTensor> tensors, int head_dim, int w)
 }
 
 // lanes of a head (4 .. 64), channels of a lane, and how many of them are read at a time: all, two or one, as width, strides and addresses
-// allow (46514 rows of 16 heads of 66, bf16: one by one 125 us forward and 199 back, by pairs 83 and 152).  8 channels where one of the types
-// is bf16, so that its pieces are 16 bytes (46514 rows of 16 heads of 128, bf16: by 4 83 us forward and 122 back, by 8 73 and 107), unless half of
+// allow (46514 rows of 16 heads, one by one and by pairs: of 34, bf16, 56 and 48 us forward, 90 and 84 back; of 66 92 and 83, but 136 and 152 back; of 250 266 and
+// 192, 360 and 336; of 66, fp32, 130 and 99, 186 and 136).  8 channels where one of the types
+// is bf16, so that its pieces are 16 bytes (46514 rows of 16 heads of 128, bf16: by 4 84 us forward and 122 back, by 8 74 and 107), unless half of
 // the lanes would have none (300000 rows of 4 heads of 16, bf16, forward: by 4 21 us, by 8 24).
 template <typename F> void with_head_shape(int head_dim, int run, F &&f)
 {
@@ -50,7 +51,7 @@ int fwd_rows(int64_t n, int heads, int groups, int pairs)
     return (int)std::max<int64_t>(rows, 1);
 }
 // Backward: the fewest that give every group a head of each kind, so that workgroups that run at once lie close together in memory (46514 rows of 16 heads of
-// 128, bf16: 4 rows 108 us, 8 rows 120, 16 rows 137), but 1024 workgroups where there are rows for them.
+// 128, bf16: 4 rows 107 us, 8 rows 112, 16 rows 130), but 1024 workgroups where there are rows for them.
 int bwd_rows(int64_t n, int heads_q, int heads_k, int others, int groups, int pairs)
 {
     int least = 1 << 30;
